@@ -207,7 +207,7 @@ def _own_dequantize(s):
 def _own_adapters(s):
     at = s["at"]
     s["sp"].adapters(s["call"], at["x"], at["down"], at["up"], at["index"], at["alpha"], at["c"], at.get("row", 0), at.get("col", 0), at["y"],
-                     at["workspace"], s["stream"])
+                     at["workspace"], s["workspace"].numel(), s["stream"])
     return {"out": s["y"][..., :s["case"]["N"]]}
 
 
