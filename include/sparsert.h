@@ -5,7 +5,8 @@
  * the sparse weight matrix A is fully known ahead of time, so it is analysed
  * once on the host (`sparsert_inspect`) and the resulting immutable plan is
  * executed many times against changing dense activations (`sparsert_spmm`,
- * `sparsert_conv3x3`).
+ * `sparsert_conv3x3`).  Around the products stand the operators that make their operands and take their
+ * results (`sparsert_rms_norm`, `sparsert_dequantize`, `sparsert_adapters`).
  *
  * Conventions used by every entry point
  *   - Matrices are C-style row-major (Section 3.2): B is K x N with N contiguous,
@@ -394,6 +395,118 @@ int sparsert_plan_load(const void *buf, size_t size, int32_t host_only, sparsert
 /* Frees the plan's host and device memory.  NULL is ignored.  The caller must
  * make sure no launch that uses the plan is still in flight. */
 void sparsert_plan_destroy(sparsert_plan *plan);
+
+/*
+ * Operators around the products of a layer, for activations laid out as the executors take them: feature-major,
+ * [rows, N] with the N tokens of a row contiguous, rows at a pitch of their own.  They make the operand of a product
+ * (sparsert_rms_norm), turn the int32 result of an int8 product into activations (sparsert_dequantize) and add what the
+ * requests of a batch have of their own beside a weight they share (sparsert_adapters).
+ *
+ * They have no plan: a descriptor says what a call works on.  Zero-initialise it, then set what you need; it is read during
+ * the call only.  Matrices are DEVICE memory of the current HIP device, 16-byte aligned; vectors of floats and indices
+ * are 4-byte aligned, so that a column slice of wider activations finds its part of them.  `stream` has to be one of the current
+ * device (EINVAL otherwise; the null stream always is).  The calls are asynchronous on `stream`, allocate nothing, do not
+ * synchronise and can be captured in a HIP graph.  No atomics: results do not change from run to run.  Operands are
+ * borrowed and must not overlap what a call writes, except where an operator names a buffer that may be the same.  Columns behind
+ * the N of a wider pitch are neither read nor written.
+ * Errors: EINVAL (null or misaligned pointer, sizes that are not positive, a pitch under N, a type the operator does not
+ * take, reserved fields set), EUNSUPPORTED (one matrix of a problem of 2 GiB and more), EHIP.
+ */
+
+/* Root-mean-square norm over the rows (features) of every column (token). */
+typedef struct sparsert_norm {
+    int32_t K, N;              /* features, tokens */
+    int32_t batch;             /* problems per call, stored back to back, 1..65535 (0 is read as 1) */
+    int32_t dtype;             /* X, R and H: SPARSERT_F32 or SPARSERT_F16 */
+    int32_t out_dtype;         /* Y: dtype, or SPARSERT_I8 */
+    int32_t ldx, ldh, ldy;     /* elements between rows of X, of R and H, of Y (0 = N, else >= N) */
+    float eps;                 /* positive and finite */
+    int32_t reserved[3];       /* must be zero */
+} sparsert_norm;
+
+/*
+ *   h[k,n] = X[k,n] + R[k,n]                              (X[k,n] if R_dev is NULL)
+ *   H[k,n] = h[k,n]                                       (if H_dev is not NULL)
+ *   v[k,n] = h[k,n] * gamma[k],  s[n] = 1 / sqrt(sum_k h[k,n]^2 / K + eps)
+ *   floating Y:  Y[k,n] = v[k,n] * s[n]
+ *   int8 Y:      a[n] = max_k |v[k,n]|,  Y[k,n] = v[k,n] * 127 / a[n] rounded to the nearest integer, ties to even,
+ *                scale[n] = a[n] * s[n] / 127:  Y[k,n] * scale[n] is the normed value, as sparsert_dequantize and
+ *                sparsert_adapters take it
+ *
+ * All of it in binary32, from the unrounded sum h; the results are rounded once.  Half results beyond its range are
+ * infinite.  int8: a column with a[n] under 2^-100 (all zeros among them) gives zeros and scale 0; one with an infinite or
+ * undefined h or v, or whose squares overflow, gives zeros and an undefined scale (NaN), which the
+ * dequantised product of the column then is as a whole.
+ *
+ *   X_dev      [batch, K, ldx]
+ *   R_dev      [batch, K, ldh] or NULL: the residual
+ *   gamma_dev  float[K] or NULL (= ones)
+ *   H_dev      [batch, K, ldh] or NULL: receives the sum; may be R_dev, and X_dev where ldh == ldx
+ *   Y_dev      [batch, K, ldy]; may be X_dev where it has its type and pitch and H_dev is another buffer; R_dev likewise
+ *   scale_dev  float[batch, N]: int8 Y only, NULL otherwise
+ */
+int sparsert_rms_norm(const sparsert_norm *norm, const void *X_dev, const void *R_dev, const float *gamma_dev,
+                      void *H_dev, void *Y_dev, float *scale_dev, void *stream);
+
+/* The int32 result of an int8 product as activations. */
+typedef struct sparsert_dequant {
+    int32_t M, N;              /* rows of the product, tokens */
+    int32_t batch;             /* problems per call, 1..65535 (0 is read as 1) */
+    int32_t dtype;             /* Y: SPARSERT_F32 or SPARSERT_F16 */
+    int32_t ldc, ldy;          /* elements between rows of C and of Y (0 = N, else >= N) */
+    int32_t reserved[2];       /* must be zero */
+} sparsert_dequant;
+
+/*
+ *   Y[m,n] = C[m,n] * col_scale[n] * row_scale[m]
+ *
+ * C as binary32 first, then one factor after the other in this order, rounded to Y's type at the store.
+ *
+ *   C_dev          int32[batch, M, ldc], what sparsert_spmm writes for an int8 plan
+ *   row_scale_dev  float[M]: the scales of the weights' rows; NULL = ones
+ *   col_scale_dev  float[batch, N]: the scales of the tokens (sparsert_rms_norm); NULL = ones
+ *   Y_dev          [batch, M, ldy]; may be C_dev for SPARSERT_F32 with ldy == ldc
+ */
+int sparsert_dequantize(const sparsert_dequant *dequant, const int32_t *C_dev, const float *row_scale_dev,
+                        const float *col_scale_dev, void *Y_dev, void *stream);
+
+/* Low-rank adapters of many requests beside a projection that they share. */
+typedef struct sparsert_adapter_set {
+    int32_t M, K, N;           /* the projection: M x K, N tokens */
+    int32_t batch;             /* problems per call, 1..65535 (0 is read as 1) */
+    int32_t rank;              /* of every adapter, 1..256; smaller ones are padded with zeros */
+    int32_t count;             /* adapters in `down` and `up` */
+    int32_t dtype;             /* down, up and Y: SPARSERT_F32 or SPARSERT_F16 */
+    int32_t x_dtype;           /* X: dtype (C then has it too), or SPARSERT_I8 (C is int32) */
+    int32_t ldx, ldc, ldy;     /* elements between rows of X, C and Y (0 = N, else >= N) */
+    int32_t reserved[3];       /* must be zero */
+} sparsert_adapter_set;
+
+/*
+ *   a = index[n]
+ *   t[j,n] = sum_k down[a][j,k] * x[k,n]
+ *   Y[m,n] = c[m,n] + alpha[a] * sum_j up[a][m,j] * t[j,n]        (c[m,n] where a is not in 0 .. count-1)
+ *
+ * where x = X and c = C or, for int8 X, x[k,n] = X[k,n] * col_scale[n] and c[m,n] = C[m,n] * col_scale[n] * row_scale[m]:
+ * the call is then given what sparsert_spmm was given and what it wrote, and takes sparsert_dequantize's place.
+ * Sums are binary32, t is kept in binary32, Y is rounded once.  A token is computed from its own column and adapter alone:
+ * what is infinite or undefined elsewhere does not reach it.
+ *
+ *   X_dev          [batch, K, ldx]
+ *   down_dev       [count, rank, K], up_dev [count, M, rank]
+ *   index_dev      int32[batch, N]: the adapter of every token; any value that names none (-1) leaves it without
+ *   alpha_dev      float[count] or NULL (= ones)
+ *   C_dev          [batch, M, ldc]: the shared projection's result
+ *   row_scale_dev  float[M], col_scale_dev float[batch, N]: int8 X only (NULL = ones), NULL otherwise
+ *   Y_dev          [batch, M, ldy]; may be C_dev where both have elements of one size and ldy == ldc
+ *   workspace_dev  DEVICE, 16-byte aligned, at least the bytes that sparsert_adapters_workspace reports (EINVAL if
+ *                  workspace_bytes is less).  Holds t between the call's two kernels, nothing from call to call: calls that
+ *                  may run at the same time (two streams, two graphs) need one each
+ */
+int sparsert_adapters_workspace(const sparsert_adapter_set *set, size_t *bytes);
+int sparsert_adapters(const sparsert_adapter_set *set, const void *X_dev, const void *down_dev, const void *up_dev,
+                      const int32_t *index_dev, const float *alpha_dev, const void *C_dev, const float *row_scale_dev,
+                      const float *col_scale_dev, void *Y_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /* Message of the last failing call on this thread ("" if none).  The pointer
  * stays valid until the next failing call on the same thread. */

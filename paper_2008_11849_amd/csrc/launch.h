@@ -1,0 +1,21 @@
+// One kernel of an operator on the caller's stream.  Host code of the .hip files.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <string>
+
+#include "plan.h"
+
+namespace sparsert {
+
+template <typename Args>
+int launch_operator(const void *kernel, dim3 grid, int threads, Args &args, void *stream, std::string &err) {
+    static_assert(sizeof(Args) <= kArgBytes, "a longer argument block costs the host more per launch");
+    void *list[] = {&args};
+    const hipError_t e = hipLaunchKernel(kernel, grid, dim3(threads), list, 0, static_cast<hipStream_t>(stream));
+    if (e == hipSuccess) return SPARSERT_OK;
+    err = std::string("hipLaunchKernel: ") + hipGetErrorString(e);
+    return SPARSERT_EHIP;
+}
+
+}  // namespace sparsert

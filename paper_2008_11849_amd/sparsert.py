@@ -33,7 +33,7 @@ INFO_COUNT = 48
 
 EXPORTED = ["sparsert_inspect", "sparsert_tune", "sparsert_spmm", "sparsert_conv3x3", "sparsert_compare_outputs", "sparsert_compare_outputs_static", "sparsert_plan_export",
             "sparsert_plan_save", "sparsert_plan_load", "sparsert_plan_destroy", "sparsert_last_error",
-            "sparsert_version"]
+            "sparsert_version", "sparsert_rms_norm", "sparsert_dequantize", "sparsert_adapters_workspace", "sparsert_adapters"]
 
 
 class Options(ctypes.Structure):
@@ -47,6 +47,20 @@ class Options(ctypes.Structure):
                 ("spec_lanes", ctypes.c_int32), ("spec_swizzle", ctypes.c_int32),
                 ("spec_vec", ctypes.c_int32), ("ldb", ctypes.c_int32), ("ldc", ctypes.c_int32),
                 ("tune_warm", ctypes.c_int32), ("spec_prefetch", ctypes.c_int32), ("reserved", ctypes.c_int32 * 2)]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("K", "N", "batch", "dtype", "out_dtype", "ldx", "ldh", "ldy")] + [
+        ("eps", ctypes.c_float), ("reserved", ctypes.c_int32 * 3)]
+
+
+class _Dequant(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("M", "N", "batch", "dtype", "ldc", "ldy")] + [("reserved", ctypes.c_int32 * 2)]
+
+
+class _AdapterSet(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("M", "K", "N", "batch", "rank", "count", "dtype", "x_dtype", "ldx", "ldc", "ldy")] + [
+        ("reserved", ctypes.c_int32 * 3)]
 
 
 TUNE_MAX = 64
@@ -113,6 +127,14 @@ _lib.sparsert_plan_load.argtypes = [_vp, ctypes.c_size_t, _i32, ctypes.POINTER(_
 _lib.sparsert_plan_load.restype = ctypes.c_int
 _lib.sparsert_plan_destroy.argtypes = [_vp]
 _lib.sparsert_plan_destroy.restype = None
+_lib.sparsert_rms_norm.argtypes = [_vp] * 8
+_lib.sparsert_rms_norm.restype = ctypes.c_int
+_lib.sparsert_dequantize.argtypes = [_vp] * 6
+_lib.sparsert_dequantize.restype = ctypes.c_int
+_lib.sparsert_adapters_workspace.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.sparsert_adapters_workspace.restype = ctypes.c_int
+_lib.sparsert_adapters.argtypes = [_vp] * 11 + [ctypes.c_size_t, _vp]
+_lib.sparsert_adapters.restype = ctypes.c_int
 _lib.sparsert_last_error.restype = ctypes.c_char_p
 _lib.sparsert_version.restype = _i32
 
@@ -272,6 +294,60 @@ def compare_outputs(plan: Plan, a_dev: int, b_dev: int, result_dev: int, stream:
 def compare_outputs_static(plan: Plan, a_dev: int, b_dev: int, result_dev: int, stream: int = 0):
     """sparsert_compare_outputs_static: the same comparison without any allocation (static scratch, no synchronisation)."""
     _check(_lib.sparsert_compare_outputs_static(plan.handle, a_dev, b_dev, result_dev, stream))
+
+
+class _Descriptor:
+    """Owner of an operator's descriptor; `handle` is its address."""
+
+    def __init__(self, fields: ctypes.Structure):
+        self.fields = fields
+        self.handle = ctypes.addressof(fields)
+
+
+class RmsNorm(_Descriptor):
+    """sparsert_norm: the sizes, types and pitches of an rms_norm call.  out_dtype: dtype unless given."""
+
+    def __init__(self, K: int, N: int, *, dtype: int = F32, out_dtype: Optional[int] = None, eps: float = 1e-6, batch: int = 0,
+                 ldx: int = 0, ldh: int = 0, ldy: int = 0):
+        super().__init__(_Norm(K, N, batch, dtype, dtype if out_dtype is None else out_dtype, ldx, ldh, ldy, eps))
+
+
+class Dequantize(_Descriptor):
+    """sparsert_dequant: the sizes, type and pitches of a dequantize call."""
+
+    def __init__(self, M: int, N: int, *, dtype: int = F32, batch: int = 0, ldc: int = 0, ldy: int = 0):
+        super().__init__(_Dequant(M, N, batch, dtype, ldc, ldy))
+
+
+class Adapters(_Descriptor):
+    """sparsert_adapter_set: the sizes, types and pitches of an adapters call.  x_dtype: dtype unless given (I8)."""
+
+    def __init__(self, M: int, K: int, N: int, rank: int, count: int, *, dtype: int = F32, x_dtype: Optional[int] = None, batch: int = 0,
+                 ldx: int = 0, ldc: int = 0, ldy: int = 0):
+        super().__init__(_AdapterSet(M, K, N, batch, rank, count, dtype, dtype if x_dtype is None else x_dtype, ldx, ldc, ldy))
+
+    def workspace_bytes(self) -> int:
+        """Device memory that a call needs to work in; calls that may run at the same time need it each."""
+        need = ctypes.c_size_t(0)
+        _check(_lib.sparsert_adapters_workspace(self.handle, ctypes.byref(need)))
+        return need.value
+
+
+def rms_norm(norm: RmsNorm, X_dev: int, R_dev: int, gamma_dev: int, H_dev: int, Y_dev: int, scale_dev: int = 0, stream: int = 0):
+    """sparsert_rms_norm: Y = norm(X + R) * gamma, H = X + R; R, gamma and H may be 0 (none); scale for an int8 Y only."""
+    _check(_lib.sparsert_rms_norm(norm.handle, X_dev, R_dev, gamma_dev, H_dev, Y_dev, scale_dev, stream))
+
+
+def dequantize(dequant: Dequantize, C_dev: int, row_scale_dev: int, col_scale_dev: int, Y_dev: int, stream: int = 0):
+    """sparsert_dequantize: Y = C * col_scale * row_scale; either scale may be 0 (ones)."""
+    _check(_lib.sparsert_dequantize(dequant.handle, C_dev, row_scale_dev, col_scale_dev, Y_dev, stream))
+
+
+def adapters(adapter_set: Adapters, X_dev: int, down_dev: int, up_dev: int, index_dev: int, alpha_dev: int, C_dev: int,
+             row_scale_dev: int, col_scale_dev: int, Y_dev: int, workspace_dev: int, workspace_bytes: int, stream: int = 0):
+    """sparsert_adapters: Y = C + alpha up (down x) of every token's adapter; alpha and, for int8 X, the scales may be 0 (ones)."""
+    _check(_lib.sparsert_adapters(adapter_set.handle, X_dev, down_dev, up_dev, index_dev, alpha_dev, C_dev, row_scale_dev, col_scale_dev,
+                                  Y_dev, workspace_dev, workspace_bytes, stream))
 
 
 # Raw entry points for callers that time launches without Python argument handling.
