@@ -132,3 +132,14 @@ def test_adapters_calls_that_are_refused():
     size = ctypes.c_size_t()
     assert sp.raw.sparsert_adapters_workspace(None, ctypes.byref(size)) == sp.EINVAL
     assert sp.raw.sparsert_adapters_workspace(adapter_set().handle, None) == sp.EINVAL
+
+
+@pytest.mark.parametrize("source", ["norm.hip", "dequantize.hip", "adapters.hip"])
+def test_wide_stores_have_no_scalar_offset(source, tmp_path):
+    """Behind a buffer store of 12 or 16 bytes with a scalar offset the compiler leaves no room before the data registers are written anew."""
+    import subprocess
+    import __graft_entry__ as entry
+    flags = [a for a in entry.hipcc_command(str(tmp_path / "kernels.s")) if not a.startswith(entry.CSRC) and a not in ("-shared", "-fPIC", "-ldl")]
+    subprocess.run(flags + ["--offload-device-only", "-S", os.path.join(entry.CSRC, source)], check=True, capture_output=True)
+    for store in re.findall(r"^\s+buffer_store_dwordx[34] (.*)", (tmp_path / "kernels.s").read_text(), re.M):
+        assert re.fullmatch(r"v\[\d+:\d+\], (v\d+|off), s\[\d+:\d+\], 0( .*)?", store.split(";")[0].strip()), store
