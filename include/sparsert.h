@@ -444,9 +444,14 @@ typedef struct sparsert_norm {
  *   H_dev      [batch, K, ldh] or NULL: receives the sum; may be R_dev, and X_dev where ldh == ldx
  *   Y_dev      [batch, K, ldy]; may be X_dev where it has its type and pitch and H_dev is another buffer; R_dev likewise
  *   scale_dev  float[batch, N]: int8 Y only, NULL otherwise
+ *   workspace_dev  DEVICE, 16-byte aligned, at least the bytes that sparsert_rms_norm_workspace reports (EINVAL if
+ *              workspace_bytes is less; 0 bytes where no workspace would be used), or NULL.  With it, columns that are too few and too long to
+ *              fill the GPU are split over it in two kernels; without it, the call is one kernel.  Holds the parts' sums between
+ *              the two, nothing from call to call: calls that may run at the same time (two streams, two graphs) need one each
  */
+int sparsert_rms_norm_workspace(const sparsert_norm *norm, size_t *bytes);
 int sparsert_rms_norm(const sparsert_norm *norm, const void *X_dev, const void *R_dev, const float *gamma_dev,
-                      void *H_dev, void *Y_dev, float *scale_dev, void *stream);
+                      void *H_dev, void *Y_dev, float *scale_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /* The int32 result of an int8 product as activations. */
 typedef struct sparsert_dequant {

@@ -1,36 +1,89 @@
 // The int32 result of an int8 product times its row and column scales.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "launch.h"
 #include "operators.h"
+#include "strips.h"
 
 namespace sparsert {
-
-namespace {
 
 struct DequantArgs {
     const int32_t *C;
     const float *row, *col;
     void *Y;
-    int32_t M, N, ldc, ldy;
+    int32_t M, N, ldc, ldy, passes;
 };
 
-template <typename T> __global__ __launch_bounds__(256) void dequantize_kernel(const DequantArgs a) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int m = (int)(i / a.N), n = (int)(i % a.N);
-    if (m >= a.M) return;
-    const float c = (float)a.C[((size_t)blockIdx.y * a.M + m) * a.ldc + n];
-    const float v = c * (a.col ? a.col[(size_t)blockIdx.y * a.N + n] : 1.0f) * (a.row ? a.row[m] : 1.0f);
-    static_cast<T *>(a.Y)[((size_t)blockIdx.y * a.M + m) * a.ldy + n] = (T)v;
+// A workgroup of 256 threads does a strip of V * L columns in `passes` * 256 / L rows: thread t has the V columns of lane t % L in the rows t / L, t / L +
+// 256 / L, ...  kDequantPasses rows are fetched before the first is scaled.
+constexpr int kDequantThreads = 256, kDequantPasses = 4;
+
+template <typename T, int V, int L> __global__ __launch_bounds__(kDequantThreads) void dequantize_kernel(const DequantArgs a) {
+    constexpr int W = V * L, ROWS = kDequantThreads / L;
+    const int strips = (a.N + W - 1) / W, blocks = (a.M + ROWS * a.passes - 1) / (ROWS * a.passes);
+    const int task = task_of(blockIdx.x, strips * blocks);
+    if (task >= strips * blocks) return;
+    const int strip = task % strips, first = task / strips * (ROWS * a.passes), end = min(a.M, first + ROWS * a.passes);
+    const int row = (int)threadIdx.x / L;
+    const Columns<V> columns(strip * W + (int)threadIdx.x % L * V, a.N);
+    const Matrix C(a.C + (int64_t)blockIdx.y * a.M * a.ldc, a.M, a.N, a.ldc, 4), Y(static_cast<T *>(a.Y) + (int64_t)blockIdx.y * a.M * a.ldy, a.M, a.N, a.ldy, sizeof(T));
+    const Matrix R(a.row, 1, a.M, a.M, 4), S(a.col ? a.col + (int64_t)blockIdx.y * a.N : nullptr, 1, a.N, a.N, 4);
+    float col[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) col[v] = 1.0f;
+    if (a.col) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float one[1];
+            load<float, 1>(S, columns.any ? (uint32_t)(columns.first + v) * 4u : kNowhere, 0, one);
+            col[v] = one[0];
+        }
+    }
+    for (int m0 = first; m0 < end; m0 += kDequantPasses * ROWS) {
+        int32_t c[kDequantPasses][V];
+        float r[kDequantPasses];
+#pragma unroll
+        for (int i = 0; i < kDequantPasses; ++i) {
+            const int m = m0 + i * ROWS + row;
+            load<int32_t, V>(C, m < end && columns.any ? ((uint32_t)m * (uint32_t)a.ldc + (uint32_t)columns.first) * 4u : kNowhere, 0, c[i]);
+            float one[1] = {1.0f};
+            if (a.row) load<float, 1>(R, m < end ? (uint32_t)m * 4u : kNowhere, 0, one);
+            r[i] = one[0];
+        }
+#pragma unroll
+        for (int i = 0; i < kDequantPasses; ++i) {
+            const int m = m0 + i * ROWS + row;
+            T y[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) y[v] = (T)((float)c[i][v] * col[v] * r[i]);
+            store<T, V>(Y, m < end && columns.any ? ((uint32_t)m * (uint32_t)a.ldy + (uint32_t)columns.first) * (uint32_t)sizeof(T) : kNowhere, 0,
+                        columns.any ? columns.skip : 0, y);
+        }
+    }
+}
+
+namespace {
+
+template <typename T, int V> const void *dequantize_of(int lanes) {
+    return lanes == 64 ? (const void *)dequantize_kernel<T, V, 64> : lanes == 16 ? (const void *)dequantize_kernel<T, V, 16>
+         : lanes == 4 ? (const void *)dequantize_kernel<T, V, 4> : (const void *)dequantize_kernel<T, V, 1>;
 }
 
 }  // namespace
 
 int launch_dequantize(const DequantCall &c, std::string &err) {
     const sparsert_dequant &d = c.d;
-    DequantArgs a{c.C, c.row, c.col, c.Y, d.M, d.N, d.ldc, d.ldy};
-    const void *kernel = d.dtype == SPARSERT_F16 ? (const void *)dequantize_kernel<_Float16> : (const void *)dequantize_kernel<float>;
-    return launch_operator(kernel, dim3((uint32_t)(((int64_t)d.M * d.N + 255) / 256), d.batch), 256, a, c.stream, err);
+    DequantArgs a{c.C, c.row, c.col, c.Y, d.M, d.N, d.ldc, d.ldy, kDequantPasses};
+    const int V = d.N < 4 ? 1 : 4;   // 16 bytes of C to a lane
+    const int vectors = (int)(((int64_t)d.N + V - 1) / V), lanes = vectors > 16 ? 64 : vectors > 4 ? 16 : vectors > 1 ? 4 : 1;
+    const int64_t strips = (vectors + lanes - 1) / lanes, rows = kDequantThreads / lanes;
+    const int64_t blocks = (d.M + rows * a.passes - 1) / (rows * a.passes), tasks = strips * blocks;
+    if (tasks >= 1ll << 30) { err = "too many workgroups"; return SPARSERT_EUNSUPPORTED; }
+    const bool half = d.dtype == SPARSERT_F16;
+    const void *kernel = V == 1 ? half ? dequantize_of<_Float16, 1>(lanes) : dequantize_of<float, 1>(lanes) : half ? dequantize_of<_Float16, 4>(lanes) : dequantize_of<float, 4>(lanes);
+    return launch_operator(kernel, dim3((uint32_t)((tasks + 7) / 8 * 8), (uint32_t)d.batch), kDequantThreads, a, c.stream, err);
 }
 
 }  // namespace sparsert

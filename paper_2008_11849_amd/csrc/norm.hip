@@ -1,6 +1,7 @@
 // Root-mean-square norm over the features of every token, with the residual's addition and, for int8 products, quantisation.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "launch.h"
@@ -16,6 +17,8 @@ struct NormArgs {
     float *scale;
     int32_t K, N, ldx, ldh, ldy;
     float eps;
+    float *sums;           // split norms: the parts' sums,
+    int32_t parts, rows;   // parts of a column, and rows of each
 };
 
 // The larger of two sizes by their bits: as numbers, and above them infinity and what is undefined.
@@ -40,69 +43,95 @@ template <int C, bool MAX> __device__ __forceinline__ float halve(float a, float
     }
 }
 
-// Column sums (or largest values) of a wave whose lanes l, l + L, l + 2 L ... hold V columns each: the lanes give half of
-// their columns away at every step, as long as they have more than one.  Returns that one; its number among the V: column_of.
-template <int V, int L, bool MAX> __device__ __forceinline__ float over_rows(const float (&v)[V], int lane) {
+// Column sums (or largest values) of a wave whose lanes l, l + L, l + 2 L ... hold V columns each.  At every step the lanes give
+// half of their columns away, as long as they have more than one; kLeft of them are left, the first of them column_of.
+template <int V, int L> constexpr int kLeft = V * L > 64 ? V * L / 64 : 1;
+template <int V, int L, bool MAX> __device__ __forceinline__ void over_rows(const float (&v)[V], int lane, float (&left)[kLeft<V, L>]) {
     float a[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) a[i] = v[i];
-    constexpr int S1 = V >= 2 ? V / 2 : 0, S2 = V >= 4 ? V / 4 : 0, S3 = V >= 8 ? V / 8 : 0;
+    constexpr int S1 = L <= 32 ? V / 2 : 0, S2 = L <= 16 ? V / 4 : 0, S3 = L <= 8 ? V / 8 : 0;
 #pragma unroll
     for (int i = 0; i < S1; ++i) a[i] = halve<32, MAX>(a[i], a[i + S1], lane);
 #pragma unroll
     for (int i = 0; i < S2; ++i) a[i] = halve<16, MAX>(a[i], a[i + S2], lane);
 #pragma unroll
     for (int i = 0; i < S3; ++i) a[i] = halve<8, MAX>(a[i], a[i + S3], lane);
-    float s = a[0];
-    if constexpr (V < 2) s = halve<32, MAX>(s, s, lane);
-    if constexpr (V < 4) s = halve<16, MAX>(s, s, lane);
-    if constexpr (V < 8 && L <= 8) s = join<MAX>(s, from_lane_xor<8>(s));
-    if constexpr (L <= 4) s = join<MAX>(s, from_lane_xor<4>(s));
-    if constexpr (L <= 2) s = join<MAX>(s, from_lane_xor<2>(s));
-    if constexpr (L <= 1) s = join<MAX>(s, from_lane_xor<1>(s));
-    return s;
+    if constexpr (V < 2 && L <= 32) a[0] = halve<32, MAX>(a[0], a[0], lane);
+    if constexpr (V < 4 && L <= 16) a[0] = halve<16, MAX>(a[0], a[0], lane);
+    if constexpr (V < 8 && L <= 8) a[0] = join<MAX>(a[0], from_lane_xor<8>(a[0]));
+    if constexpr (L <= 4) a[0] = join<MAX>(a[0], from_lane_xor<4>(a[0]));
+    if constexpr (L <= 2) a[0] = join<MAX>(a[0], from_lane_xor<2>(a[0]));
+    if constexpr (L <= 1) a[0] = join<MAX>(a[0], from_lane_xor<1>(a[0]));
+#pragma unroll
+    for (int i = 0; i < kLeft<V, L>; ++i) left[i] = a[i];
 }
-template <int V> __device__ __forceinline__ int column_of(int lane) { return V == 8 ? lane >> 3 & 7 : V == 4 ? lane >> 4 & 3 : V == 2 ? lane >> 5 : 0; }
-// of the lanes with the same sum, the one that stores it
-template <int V, int L> __device__ __forceinline__ bool stores(int lane) { return (lane & (64 / V - 1)) < L; }
+template <int V, int L> __device__ __forceinline__ int column_of(int lane) {
+    int c = 0;
+    if (V >= 2 && L <= 32) c += (lane >> 5 & 1) * (V / 2);
+    if (V >= 4 && L <= 16) c += (lane >> 4 & 1) * (V / 4);
+    if (V >= 8 && L <= 8) c += (lane >> 3 & 1) * (V / 8);
+    return c;
+}
+// of the lanes with the same sums, the one that stores them
+template <int V, int L> __device__ __forceinline__ bool stores(int lane) { return V * L >= 64 || (lane & (64 / V - 1)) < L; }
+// The sums of a wave's lanes into its row of `to`, one for each column of the strip.
+template <int V, int L, bool MAX> __device__ __forceinline__ void wave_sums(const float (&v)[V], int lane, int skip, float *to) {
+    float left[kLeft<V, L>];
+    over_rows<V, L, MAX>(v, lane, left);
+    if (stores<V, L>(lane))
+#pragma unroll
+        for (int i = 0; i < kLeft<V, L>; ++i) {
+            const int c = column_of<V, L>(lane) + i;
+            if (c >= skip) to[lane % L * V + c - skip] = left[i];
+        }
+}
 
-// A workgroup of THREADS threads does a strip of V * L columns: thread t has the V columns of lane t % L in the rows t / L, t / L +
-// THREADS / L, ...  PASSES of them are fetched at a time, all before the first is used.  HELD: they are all rows, and stay in
-// registers; otherwise the rows are fetched twice, once for the sums and once for the results.
-// WHOLE: every lane's V columns exist, as in all strips but a last one.
-template <typename T, bool QUANT, int V, int L, int PASSES, bool HELD, int THREADS, bool WHOLE>
-__device__ __forceinline__ void norm_strip(const NormArgs &a, int strip) {
-    constexpr int W = V * L, WAVES = THREADS / 64, ROWS = THREADS / L;
-    __shared__ __align__(16) float sums[WAVES][W], tops[QUANT ? WAVES : 1][W], factors[W];
-    typedef typename std::conditional<QUANT, int8_t, T>::type Out;
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, row = t / L, n = strip * W + t % L * V;
-    const int valid = WHOLE ? V : a.N - n;   // columns of this lane; none (not positive) behind the last one
-    const Matrix X(static_cast<const T *>(a.X) + (int64_t)blockIdx.y * a.K * a.ldx, a.K, a.N, a.ldx, sizeof(T));
-    const Matrix R(a.R ? static_cast<const T *>(a.R) + (int64_t)blockIdx.y * a.K * a.ldh : nullptr, a.K, a.N, a.ldh, sizeof(T));
-    const Matrix H(a.H ? static_cast<T *>(a.H) + (int64_t)blockIdx.y * a.K * a.ldh : nullptr, a.K, a.N, a.ldh, sizeof(T));
-    const Matrix Y(static_cast<Out *>(a.Y) + (int64_t)blockIdx.y * a.K * a.ldy, a.K, a.N, a.ldy, sizeof(Out));
-    const Matrix G(a.gamma, 1, a.K, a.K, sizeof(float));
+// What a column's weighted sums are multiplied with, from the sum of its squares and its largest |h * gamma|.
+template <bool QUANT> __device__ __forceinline__ float factor_of(float total, float most, const NormArgs &a, float &scale) {
+    const float inv = 1.0f / sqrtf(total / (float)a.K + a.eps);
+    if constexpr (!QUANT) return inv;
+    const bool sound = total < INFINITY && most < INFINITY, some = most >= 0x1p-100f;
+    scale = !sound ? NAN : some ? most * inv / 127.0f : 0.0f;
+    return sound && some ? 127.0f / most : 0.0f;
+}
+template <typename Out> __device__ __forceinline__ Out result(float v, float f) {
+    if constexpr (sizeof(Out) == 1) return f == 0.0f ? (int8_t)0 : (int8_t)(int)rintf(v * f);
+    else return (Out)(v * f);
+}
 
-    float h[PASSES][V], g[PASSES];
-    auto place = [&](int k0, int i, int ld, int size, uint32_t &common) {   // this lane's byte in pass i of the rows from k0 on
-        const int first = k0 + i * ROWS;
-        common = first < a.K ? (uint32_t)first * (uint32_t)ld * (uint32_t)size : 0;
-        return first + row < a.K && valid > 0 ? ((uint32_t)row * (uint32_t)ld + (uint32_t)n) * (uint32_t)size : kNowhere;
-    };
-    auto fetch = [&](int k0) {
+// Rows [first, end) of a strip of V * L columns: thread t has V columns in the rows first + t / L, first + t / L + THREADS / L, ...,
+// a pass for each of them.
+template <typename T, int V, int L, int THREADS> struct Rows {
+    static constexpr int W = V * L, ROWS = THREADS / L;
+    const NormArgs &a;
+    int row, first, end;
+    Columns<V> columns;
+    Matrix X, R, G;
+    __device__ __forceinline__ Rows(const NormArgs &a, int strip, int first, int end)
+        : a(a), row((int)threadIdx.x / L), first(first), end(end), columns(strip * W + (int)threadIdx.x % L * V, a.N),
+          X(static_cast<const T *>(a.X) + (int64_t)blockIdx.y * a.K * a.ldx, a.K, a.N, a.ldx, sizeof(T)),
+          R(a.R ? static_cast<const T *>(a.R) + (int64_t)blockIdx.y * a.K * a.ldh : nullptr, a.K, a.N, a.ldh, sizeof(T)), G(a.gamma, 1, a.K, a.K, sizeof(float)) {}
+    // This thread's byte in pass i of the rows from k0 on.
+    __device__ __forceinline__ uint32_t place(int k0, int i, int ld, int size, uint32_t &common) const {
+        const int at = k0 + i * ROWS;
+        common = at < end ? (uint32_t)at * (uint32_t)ld * (uint32_t)size : 0;
+        return at + row < end && columns.any ? ((uint32_t)row * (uint32_t)ld + (uint32_t)columns.first) * (uint32_t)size : kNowhere;
+    }
+    // The sums and weights of PASSES passes, every load before the first use.  Rows past the end are zeros.
+    template <int PASSES> __device__ __forceinline__ void fetch(int k0, float (&h)[PASSES][V], float (&g)[PASSES]) const {
         T x[PASSES][V], r[PASSES][V];
+        uint32_t common;
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
-            uint32_t common;
             const uint32_t at = place(k0, i, a.ldx, sizeof(T), common);
-            load<T, V>(X, at, common, valid, x[i]);
+            load<T, V>(X, at, common, x[i]);
         }
         if (a.R) {
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
-                uint32_t common;
                 const uint32_t at = place(k0, i, a.ldh, sizeof(T), common);
-                load<T, V>(R, at, common, valid, r[i]);
+                load<T, V>(R, at, common, r[i]);
             }
         } else {
 #pragma unroll
@@ -113,113 +142,206 @@ __device__ __forceinline__ void norm_strip(const NormArgs &a, int strip) {
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
             const int k = k0 + i * ROWS + row;
-            g[i] = a.gamma ? __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(G.at, k < a.K ? (uint32_t)k * 4u : kNowhere, 0, 0)) : 1.0f;
+            g[i] = a.gamma ? __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(G.at, k < end ? (uint32_t)k * 4u : kNowhere, 0, 0)) : 1.0f;
         }
 #pragma unroll
         for (int i = 0; i < PASSES; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) h[i][v] = (float)x[i][v] + (float)r[i][v];
-    };
-    auto write_sum = [&](int k0) {
-        if (!a.H) return;
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            T out[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) out[v] = (T)h[i][v];
-            uint32_t common;
-            const uint32_t at = place(k0, i, a.ldh, sizeof(T), common);
-            store<T, V>(H, at, common, valid, out);
-        }
-    };
-    float s[V], top[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) s[v] = top[v] = 0.0f;
-    auto add_up_and_weigh = [&]() {   // h becomes h * gamma
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i)
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                s[v] = __builtin_fmaf(h[i][v], h[i][v], s[v]);
-                h[i][v] *= g[i];
-                if constexpr (QUANT) top[v] = larger(top[v], fabsf(h[i][v]));
-            }
-    };
-    float f[V];
-    auto write = [&](int k0) {
+    }
+    template <typename Out, int PASSES, typename F> __device__ __forceinline__ void write(const Matrix &m, int k0, int ld, F value) const {
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
             Out out[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if constexpr (QUANT) out[v] = f[v] == 0.0f ? (int8_t)0 : (int8_t)(int)rintf(h[i][v] * f[v]);
-                else out[v] = (T)(h[i][v] * f[v]);
-            }
+            for (int v = 0; v < V; ++v) out[v] = value(i, v);
             uint32_t common;
-            const uint32_t at = place(k0, i, a.ldy, sizeof(Out), common);
-            store<Out, V>(Y, at, common, valid, out);
+            const uint32_t at = place(k0, i, ld, sizeof(Out), common);
+            store<Out, V>(m, at, common, columns.any ? columns.skip : 0, out);
         }
+    }
+};
+
+template <typename T, bool QUANT> using out_t = typename std::conditional<QUANT, int8_t, T>::type;
+template <typename T> __device__ __forceinline__ Matrix sum_of(const NormArgs &a) { return Matrix(a.H ? static_cast<T *>(a.H) + (int64_t)blockIdx.y * a.K * a.ldh : nullptr, a.K, a.N, a.ldh, sizeof(T)); }
+template <typename Out> __device__ __forceinline__ Matrix result_of(const NormArgs &a) { return Matrix(static_cast<Out *>(a.Y) + (int64_t)blockIdx.y * a.K * a.ldy, a.K, a.N, a.ldy, sizeof(Out)); }
+
+// ---- One kernel: a workgroup of THREADS threads does a strip.  HELD: PASSES passes are all rows, and stay in registers between the
+// sums and the results; otherwise the rows are fetched twice.
+template <typename T, bool QUANT, int V, int L, int PASSES, bool HELD, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs a) {
+    typedef out_t<T, QUANT> Out;
+    typedef Rows<T, V, L, THREADS> Strip;
+    constexpr int W = V * L, WAVES = THREADS / 64, ROWS = Strip::ROWS;
+    __shared__ __align__(16) float sums[WAVES][W], tops[QUANT ? WAVES : 1][W], factors[W];
+    const int strips = (a.N + W - 1) / W, strip = task_of(blockIdx.x, strips);
+    if (strip >= strips) return;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const Strip rows(a, strip, 0, a.K);
+    const Matrix H = sum_of<T>(a), Y = result_of<Out>(a);
+    float h[PASSES][V], g[PASSES], s[V], top[V], f[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[v] = top[v] = 0.0f;
+    auto weigh = [&](bool add) {   // h becomes h * gamma; `add`: and is added up
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (add) s[v] = __builtin_fmaf(h[i][v], h[i][v], s[v]);
+                h[i][v] *= g[i];
+                if constexpr (QUANT)
+                    if (add) top[v] = larger(top[v], fabsf(h[i][v]));
+            }
     };
+    auto write_sum = [&](int k0) {
+        if (a.H) rows.template write<T, PASSES>(H, k0, a.ldh, [&](int i, int v) { return (T)h[i][v]; });
+    };
+    auto write = [&](int k0) { rows.template write<Out, PASSES>(Y, k0, a.ldy, [&](int i, int v) { return result<Out>(h[i][v], f[v]); }); };
 
     if constexpr (HELD) {
-        fetch(0);
+        rows.fetch(0, h, g);
         write_sum(0);
-        add_up_and_weigh();
+        weigh(true);
     } else {
         for (int k0 = 0; k0 < a.K; k0 += PASSES * ROWS) {
-            fetch(k0);
-            add_up_and_weigh();
+            rows.fetch(k0, h, g);
+            weigh(true);
         }
     }
-    // Rows past K are zeros: they add nothing.  The sums meet in LDS, in wave order.
-    const float mine = over_rows<V, L, false>(s, lane);
-    float largest = 0.0f;
-    if constexpr (QUANT) largest = over_rows<V, L, true>(top, lane);
-    if (stores<V, L>(lane)) {
-        sums[wave][lane % L * V + column_of<V>(lane)] = mine;
-        if constexpr (QUANT) tops[wave][lane % L * V + column_of<V>(lane)] = largest;
-    }
+    // The sums meet in LDS, in wave order.
+    wave_sums<V, L, false>(s, lane, rows.columns.skip, sums[wave]);
+    if constexpr (QUANT) wave_sums<V, L, true>(top, lane, rows.columns.skip, tops[wave]);
     __syncthreads();
-    if (t < W) {
-        float total = sums[0][t], most = 0.0f;
+    if (t < W && strip * W + t < a.N) {
+        float total = sums[0][t], most = 0.0f, scale;
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) total += sums[w][t];
-        const float inv = 1.0f / sqrtf(total / (float)a.K + a.eps);
-        float factor = inv;
-        if constexpr (QUANT) {
+        if constexpr (QUANT)
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) most = larger(most, tops[w][t]);
-            const bool sound = total < INFINITY && most < INFINITY, some = most >= 0x1p-100f;
-            factor = sound && some ? 127.0f / most : 0.0f;
-            if (strip * W + t < a.N) a.scale[(size_t)blockIdx.y * a.N + strip * W + t] = !sound ? NAN : some ? most * inv / 127.0f : 0.0f;
-        }
-        factors[t] = factor;
+        factors[t] = factor_of<QUANT>(total, most, a, scale);
+        if constexpr (QUANT) a.scale[(size_t)blockIdx.y * a.N + strip * W + t] = scale;
     }
     __syncthreads();
 #pragma unroll
-    for (int v = 0; v < V; ++v) f[v] = factors[t % L * V + v];
+    for (int v = 0; v < V; ++v) f[v] = factors[max(0, t % L * V + v - rows.columns.skip)];   // (of skipped columns: not used)
     if constexpr (HELD) {
         write(0);
     } else {
         for (int k0 = 0; k0 < a.K; k0 += PASSES * ROWS) {
-            fetch(k0);
+            rows.fetch(k0, h, g);
             write_sum(k0);
-#pragma unroll
-            for (int i = 0; i < PASSES; ++i)
-#pragma unroll
-                for (int v = 0; v < V; ++v) h[i][v] *= g[i];
+            weigh(false);
             write(k0);
         }
     }
 }
 
-template <typename T, bool QUANT, int V, int L, int PASSES, bool HELD, int THREADS>
-__global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs a) {
-    constexpr int W = V * L;
-    const int strips = (a.N + W - 1) / W, strip = task_of(blockIdx.x, strips);
-    if (strip >= strips) return;
-    if (V == 1 || strip * W + W <= a.N) norm_strip<T, QUANT, V, L, PASSES, HELD, THREADS, V != 1>(a, strip);
-    else if constexpr (V != 1) norm_strip<T, QUANT, V, L, PASSES, HELD, THREADS, false>(a, strip);
+// ---- Two kernels, for columns too few and too long to fill the GPU: sums of every part of a strip, then the results.  A part is
+// `rows` rows of a strip.  The parts' sums and largest values lie in the caller's workspace, [batch][part][1 or 2][N].
+constexpr int kPartThreads = 256, kWideLanes = 16;
+constexpr int kPartPasses = 4;    // rows of a thread that are fetched at a time
+constexpr int kPartsAtOnce = 8;   // sums that a thread of the second kernel fetches at a time
+
+// Task -> strip and part, the same in both kernels, so that the second one finds in its L2 what the first one fetched.  Parts of a strip
+// one after the other; in the wide strips that calls beyond the caches take, strips of a part, so that an XCD reads long runs of a row.
+template <int L> __device__ __forceinline__ int strip_of(int task, int strips, int parts) { return L >= kWideLanes ? task % strips : task / parts; }
+template <int L> __device__ __forceinline__ int part_of(int task, int strips, int parts) { return L >= kWideLanes ? task / strips : task % parts; }
+
+template <typename T, bool QUANT, int V, int L> __global__ __launch_bounds__(kPartThreads) void norm_sums_kernel(const NormArgs a) {
+    typedef Rows<T, V, L, kPartThreads> Part;
+    constexpr int W = V * L, WAVES = kPartThreads / 64;
+    __shared__ float sums[WAVES][W], tops[QUANT ? WAVES : 1][W];
+    const int strips = (a.N + W - 1) / W, task = task_of(blockIdx.x, strips * a.parts);
+    if (task >= strips * a.parts) return;
+    const int strip = strip_of<L>(task, strips, a.parts), part = part_of<L>(task, strips, a.parts), t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const Part p(a, strip, part * a.rows, min(a.K, (part + 1) * a.rows));
+    float s[V], top[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[v] = top[v] = 0.0f;
+    for (int k0 = p.first; k0 < p.end; k0 += kPartPasses * Part::ROWS) {
+        float h[kPartPasses][V], g[kPartPasses];
+        p.fetch(k0, h, g);
+#pragma unroll
+        for (int i = 0; i < kPartPasses; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                s[v] = __builtin_fmaf(h[i][v], h[i][v], s[v]);
+                if constexpr (QUANT) top[v] = larger(top[v], fabsf(h[i][v] * g[i]));
+            }
+    }
+    wave_sums<V, L, false>(s, lane, p.columns.skip, sums[wave]);
+    if constexpr (QUANT) wave_sums<V, L, true>(top, lane, p.columns.skip, tops[wave]);
+    __syncthreads();
+    float *const to = a.sums + ((size_t)blockIdx.y * a.parts + part) * (QUANT ? 2 : 1) * a.N;
+    const int n = strip * W + t;
+    if (t < W && n < a.N) {
+        float total = sums[0][t], most = 0.0f;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) total += sums[w][t];
+        to[n] = total;
+        if constexpr (QUANT) {
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) most = larger(most, tops[w][t]);
+            to[a.N + n] = most;
+        }
+    }
+}
+
+template <typename T, bool QUANT, int V, int L> __global__ __launch_bounds__(kPartThreads) void norm_results_kernel(const NormArgs a) {
+    typedef out_t<T, QUANT> Out;
+    typedef Rows<T, V, L, kPartThreads> Part;
+    constexpr int W = V * L, GROUPS = kPartThreads / W;
+    __shared__ float sums[GROUPS][W], tops[QUANT ? GROUPS : 1][W];
+    __shared__ __align__(16) float factors[W];
+    const int strips = (a.N + W - 1) / W, task = task_of(blockIdx.x, strips * a.parts);
+    if (task >= strips * a.parts) return;
+    const int strip = strip_of<L>(task, strips, a.parts), part = part_of<L>(task, strips, a.parts), t = threadIdx.x;
+    const Part p(a, strip, part * a.rows, min(a.K, (part + 1) * a.rows));
+    const Matrix H = sum_of<T>(a), Y = result_of<Out>(a);
+    // The parts' sums of a column, dealt to GROUPS threads and joined in LDS: always in the same order.
+    const float *const from = a.sums + (size_t)blockIdx.y * a.parts * (QUANT ? 2 : 1) * a.N;
+    const int c = t % W, n = strip * W + c;
+    float total = 0.0f, most = 0.0f;
+    if (n < a.N)
+        for (int of = t / W; of < a.parts; of += GROUPS * kPartsAtOnce) {
+            float u[kPartsAtOnce], q[kPartsAtOnce];
+#pragma unroll
+            for (int j = 0; j < kPartsAtOnce; ++j) {
+                const int which = of + j * GROUPS;
+                u[j] = which < a.parts ? from[(size_t)which * (QUANT ? 2 : 1) * a.N + n] : 0.0f;
+                if constexpr (QUANT) q[j] = which < a.parts ? from[((size_t)which * 2 + 1) * a.N + n] : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < kPartsAtOnce; ++j) {
+                total += u[j];
+                if constexpr (QUANT) most = larger(most, q[j]);
+            }
+        }
+    sums[t / W][c] = total;
+    if constexpr (QUANT) tops[t / W][c] = most;
+    __syncthreads();
+    if (t < W) {
+        float scale;
+#pragma unroll
+        for (int i = 1; i < GROUPS; ++i) {
+            total += sums[i][c];
+            if constexpr (QUANT) most = larger(most, tops[i][c]);
+        }
+        factors[t] = factor_of<QUANT>(total, most, a, scale);
+        if constexpr (QUANT)
+            if (part == 0 && n < a.N) a.scale[(size_t)blockIdx.y * a.N + n] = scale;
+    }
+    __syncthreads();
+    float f[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) f[v] = factors[max(0, t % L * V + v - p.columns.skip)];   // (of skipped columns: not used)
+    for (int k0 = p.first; k0 < p.end; k0 += kPartPasses * Part::ROWS) {
+        float h[kPartPasses][V], g[kPartPasses];
+        p.fetch(k0, h, g);
+        if (a.H) p.template write<T, kPartPasses>(H, k0, a.ldh, [&](int i, int v) { return (T)h[i][v]; });
+        p.template write<Out, kPartPasses>(Y, k0, a.ldy, [&](int i, int v) { return result<Out>(h[i][v] * g[i], f[v]); });
+    }
 }
 
 namespace {
@@ -236,24 +358,82 @@ template <typename T, bool QUANT, int V, int L> const void *norm_of(int K) {
     return (const void *)norm_kernel<T, QUANT, V, L, 4, false, kNormThreads>;
 }
 
-template <typename T, bool QUANT> const void *norm_of(const sparsert_norm &d, int &columns) {
-    constexpr int V = 16 / sizeof(T);   // columns of a lane: 16 bytes
+// Columns of a lane and lanes of a strip: 16 bytes, and as many lanes as leave 256 workgroups; narrower than that, one column to a lane.
+template <typename T> void strip_shape(const sparsert_norm &d, int &V, int &L) {
+    V = 16 / sizeof(T);
     if (d.N < V) {
-        const int lanes = d.N > 4 ? 8 : d.N > 2 ? 4 : d.N;
-        columns = lanes;
-        return lanes == 8 ? norm_of<T, QUANT, 1, 8>(d.K) : lanes == 4 ? norm_of<T, QUANT, 1, 4>(d.K) : lanes == 2 ? norm_of<T, QUANT, 1, 2>(d.K) : norm_of<T, QUANT, 1, 1>(d.K);
+        V = 1;
+        L = d.N > 4 ? 8 : d.N > 2 ? 4 : d.N;
+        return;
     }
     const int64_t vectors = (int64_t)d.batch * ((d.N + V - 1) / V);
-    const int lanes = vectors >= 8 * 256 ? 8 : vectors >= 4 * 256 ? 4 : vectors >= 2 * 256 ? 2 : 1;
-    columns = lanes * V;
-    return lanes == 8 ? norm_of<T, QUANT, V, 8>(d.K) : lanes == 4 ? norm_of<T, QUANT, V, 4>(d.K) : lanes == 2 ? norm_of<T, QUANT, V, 2>(d.K) : norm_of<T, QUANT, V, 1>(d.K);
+    L = vectors >= 8 * 256 ? 8 : vectors >= 4 * 256 ? 4 : vectors >= 2 * 256 ? 2 : 1;
+}
+
+template <typename T, bool QUANT> const void *norm_of(const sparsert_norm &d, int &columns) {
+    int V, L;
+    strip_shape<T>(d, V, L);
+    columns = V * L;
+    if (V == 1) return L == 8 ? norm_of<T, QUANT, 1, 8>(d.K) : L == 4 ? norm_of<T, QUANT, 1, 4>(d.K) : L == 2 ? norm_of<T, QUANT, 1, 2>(d.K) : norm_of<T, QUANT, 1, 1>(d.K);
+    constexpr int W = 16 / sizeof(T);
+    return L == 8 ? norm_of<T, QUANT, W, 8>(d.K) : L == 4 ? norm_of<T, QUANT, W, 4>(d.K) : L == 2 ? norm_of<T, QUANT, W, 2>(d.K) : norm_of<T, QUANT, W, 1>(d.K);
+}
+
+// Estimate of a call as one kernel.
+template <typename T> double one_kernel_us(const sparsert_norm &d, double bytes) {
+    int V, L;
+    strip_shape<T>(d, V, L);
+    const int passes = (d.K + kNormThreads / L - 1) / (kNormThreads / L);
+    if (V == 1) return 2.2 + passes * (passes <= 8 ? 0.2 : 0.55);
+    const double lines = std::min(1.0, d.ldx * (double)sizeof(T) / 128.0);   // that a lane's vector is alone in
+    return 2.2 + passes * (0.35 + 1.9 * lines / L) * (passes <= 8 ? 1.0 : 2.0) + bytes / 5e6;
+}
+
+struct SplitNorm { int parts, rows, strips; const void *sums, *results; };
+
+template <typename T, bool QUANT, int V, int L> SplitNorm split_with(const sparsert_norm &d, int workgroups) {
+    constexpr int W = V * L, ROWS = kPartThreads / L;
+    const int strips = (int)(((int64_t)d.N + W - 1) / W);
+    // No more parts than a workgroup fetches the sums of at once.
+    const int64_t most = std::min<int64_t>((d.K + ROWS - 1) / ROWS, kPartThreads / W * kPartsAtOnce);
+    const int64_t parts = std::min(most, std::max<int64_t>(1, workgroups / ((int64_t)strips * d.batch)));
+    const int rows = (int)((d.K + parts - 1) / parts);
+    return {(d.K + rows - 1) / rows, rows, strips, (const void *)norm_sums_kernel<T, QUANT, V, L>, (const void *)norm_results_kernel<T, QUANT, V, L>};
+}
+
+template <typename T, bool QUANT> SplitNorm split_of(const sparsert_norm &d) {
+    constexpr int V = 16 / sizeof(T);
+    const double bytes = (double)d.K * d.N * d.batch * (3 * sizeof(T) + sizeof(out_t<T, QUANT>));
+    if (one_kernel_us<T>(d, bytes) <= (QUANT ? 6.2 : 5.3) + bytes / 4.4e6) return {};
+    if (d.N < V) return d.N > 4 ? split_with<T, QUANT, 1, 8>(d, 256) : d.N > 2 ? split_with<T, QUANT, 1, 4>(d, 256) : split_with<T, QUANT, 1, 2>(d, 256);
+    constexpr int64_t wide = V * kWideLanes;
+    if (bytes > 40e6 && d.batch * (d.N / wide) * (kPartThreads / wide * kPartsAtOnce) >= 256) return split_with<T, QUANT, V, kWideLanes>(d, 512);
+    return d.N > 4 * V ? split_with<T, QUANT, V, 8>(d, 256) : d.N > 2 * V ? split_with<T, QUANT, V, 4>(d, 256)
+         : d.N > V ? split_with<T, QUANT, V, 2>(d, 256) : split_with<T, QUANT, V, 1>(d, 256);
+}
+
+SplitNorm split_norm(const sparsert_norm &d) {
+    const bool half = d.dtype == SPARSERT_F16, quant = d.out_dtype == SPARSERT_I8;
+    return half ? quant ? split_of<_Float16, true>(d) : split_of<_Float16, false>(d) : quant ? split_of<float, true>(d) : split_of<float, false>(d);
 }
 
 }  // namespace
 
+size_t norm_workspace(const sparsert_norm &d) {
+    const SplitNorm s = split_norm(d);
+    return s.parts ? (size_t)d.batch * s.parts * (d.out_dtype == SPARSERT_I8 ? 2 : 1) * d.N * sizeof(float) : 0;
+}
+
 int launch_norm(const NormCall &c, std::string &err) {
     const sparsert_norm &d = c.d;
-    NormArgs a{c.X, c.R, c.gamma, c.H, c.Y, c.scale, d.K, d.N, d.ldx, d.ldh, d.ldy, d.eps};
+    NormArgs a{c.X, c.R, c.gamma, c.H, c.Y, c.scale, d.K, d.N, d.ldx, d.ldh, d.ldy, d.eps, c.workspace, 0, 0};
+    if (c.workspace)
+        if (const SplitNorm s = split_norm(d); s.parts) {
+            a.parts = s.parts; a.rows = s.rows;
+            const dim3 grid((uint32_t)((s.strips * s.parts + 7) / 8 * 8), (uint32_t)d.batch);
+            if (int rc = launch_operator(s.sums, grid, kPartThreads, a, c.stream, err)) return rc;
+            return launch_operator(s.results, grid, kPartThreads, a, c.stream, err);
+        }
     int columns = 1;
     const bool half = d.dtype == SPARSERT_F16, quant = d.out_dtype == SPARSERT_I8;
     const void *kernel = half ? quant ? norm_of<_Float16, true>(d, columns) : norm_of<_Float16, false>(d, columns)

@@ -38,6 +38,16 @@ int check_stream(void *stream) {
     return sparsert::stream_of_current_device(stream) ? SPARSERT_OK : set_error(SPARSERT_EINVAL, "the stream is not one of the current HIP device");
 }
 
+int check_norm(sparsert_norm &d) {
+    if (int rc = check_sizes(d.K, d.N, d.batch, d.reserved, 3)) return rc;
+    if (!floating(d.dtype)) return set_error(SPARSERT_EINVAL, "dtype must be F32 or F16");
+    if (d.out_dtype != d.dtype && d.out_dtype != SPARSERT_I8) return set_error(SPARSERT_EINVAL, "out_dtype must be dtype or I8");
+    if (!(d.eps > 0.0f) || !std::isfinite(d.eps)) return set_error(SPARSERT_EINVAL, "eps must be positive and finite");
+    if (int rc = check_pitch(d.ldx, d.K, d.N, size_of(d.dtype), "ldx")) return rc;
+    if (int rc = check_pitch(d.ldh, d.K, d.N, size_of(d.dtype), "ldh")) return rc;
+    return check_pitch(d.ldy, d.K, d.N, size_of(d.out_dtype), "ldy");
+}
+
 int check_set(sparsert_adapter_set &d) {
     if (int rc = check_sizes(d.M, d.N, d.batch, d.reserved, 3)) return rc;
     if (d.K < 1) return set_error(SPARSERT_EINVAL, "sizes must be positive");
@@ -71,27 +81,33 @@ template <typename F> int guarded(F f) {
 
 extern "C" {
 
+int sparsert_rms_norm_workspace(const sparsert_norm *norm, size_t *bytes) {
+    return guarded([&](std::string &) {
+        if (!norm || !bytes) return set_error(SPARSERT_EINVAL, "norm or bytes is NULL");
+        *bytes = 0;
+        sparsert_norm d = *norm;
+        if (int rc = check_norm(d)) return rc;
+        *bytes = sparsert::norm_workspace(d);
+        return (int)SPARSERT_OK;
+    });
+}
+
 int sparsert_rms_norm(const sparsert_norm *norm, const void *X_dev, const void *R_dev, const float *gamma_dev, void *H_dev, void *Y_dev,
-                      float *scale_dev, void *stream) {
+                      float *scale_dev, void *workspace_dev, size_t workspace_bytes, void *stream) {
     return guarded([&](std::string &err) {
         if (!norm) return set_error(SPARSERT_EINVAL, "norm is NULL");
-        sparsert::NormCall c{*norm, X_dev, R_dev, gamma_dev, H_dev, Y_dev, scale_dev, stream};
+        sparsert::NormCall c{*norm, X_dev, R_dev, gamma_dev, H_dev, Y_dev, scale_dev, static_cast<float *>(workspace_dev), stream};
         sparsert_norm &d = c.d;
-        if (int rc = check_sizes(d.K, d.N, d.batch, d.reserved, 3)) return rc;
-        if (!floating(d.dtype)) return set_error(SPARSERT_EINVAL, "dtype must be F32 or F16");
-        if (d.out_dtype != d.dtype && d.out_dtype != SPARSERT_I8) return set_error(SPARSERT_EINVAL, "out_dtype must be dtype or I8");
-        if (!(d.eps > 0.0f) || !std::isfinite(d.eps)) return set_error(SPARSERT_EINVAL, "eps must be positive and finite");
-        if (int rc = check_pitch(d.ldx, d.K, d.N, size_of(d.dtype), "ldx")) return rc;
-        if (int rc = check_pitch(d.ldh, d.K, d.N, size_of(d.dtype), "ldh")) return rc;
-        if (int rc = check_pitch(d.ldy, d.K, d.N, size_of(d.out_dtype), "ldy")) return rc;
+        if (int rc = check_norm(d)) return rc;
         if (!X_dev || !Y_dev) return set_error(SPARSERT_EINVAL, "device pointer is NULL");
         if ((d.out_dtype == SPARSERT_I8) != (scale_dev != nullptr)) return set_error(SPARSERT_EINVAL, "scale_dev goes with an int8 result, and only with one");
-        if (misaligned(15, X_dev, R_dev, H_dev, Y_dev)) return set_error(SPARSERT_EINVAL, "matrices must be 16-byte aligned");
+        if (misaligned(15, X_dev, R_dev, H_dev, Y_dev, workspace_dev)) return set_error(SPARSERT_EINVAL, "matrices and workspace must be 16-byte aligned");
         if (misaligned(3, gamma_dev, scale_dev)) return set_error(SPARSERT_EINVAL, "vectors must be 4-byte aligned");
         if (Y_dev == H_dev) return set_error(SPARSERT_EINVAL, "Y and H must be two buffers");
         if (H_dev == X_dev && d.ldh != d.ldx) return set_error(SPARSERT_EINVAL, "H may be X only at the same pitch");
         if (Y_dev == X_dev && (d.out_dtype != d.dtype || d.ldy != d.ldx)) return set_error(SPARSERT_EINVAL, "Y may be X only with its type and pitch");
         if (Y_dev == R_dev && (d.out_dtype != d.dtype || d.ldy != d.ldh)) return set_error(SPARSERT_EINVAL, "Y may be R only with its type and pitch");
+        if (workspace_dev && workspace_bytes < sparsert::norm_workspace(d)) return set_error(SPARSERT_EINVAL, "the workspace is smaller than sparsert_rms_norm_workspace says");
         if (int rc = check_stream(stream)) return rc;
         return sparsert::launch_norm(c, err);
     });

@@ -19,9 +19,10 @@ struct NormCall {
     const void *X, *R;
     const float *gamma;
     void *H, *Y;
-    float *scale;
+    float *scale, *workspace;   // workspace: NULL or norm_workspace bytes
     void *stream;
 };
+size_t norm_workspace(const sparsert_norm &d);
 int launch_norm(const NormCall &c, std::string &err);
 
 struct DequantCall {

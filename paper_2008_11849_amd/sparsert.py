@@ -33,7 +33,7 @@ INFO_COUNT = 48
 
 EXPORTED = ["sparsert_inspect", "sparsert_tune", "sparsert_spmm", "sparsert_conv3x3", "sparsert_compare_outputs", "sparsert_compare_outputs_static", "sparsert_plan_export",
             "sparsert_plan_save", "sparsert_plan_load", "sparsert_plan_destroy", "sparsert_last_error",
-            "sparsert_version", "sparsert_rms_norm", "sparsert_dequantize", "sparsert_adapters_workspace", "sparsert_adapters"]
+            "sparsert_version", "sparsert_rms_norm_workspace", "sparsert_rms_norm", "sparsert_dequantize", "sparsert_adapters_workspace", "sparsert_adapters"]
 
 
 class Options(ctypes.Structure):
@@ -127,7 +127,9 @@ _lib.sparsert_plan_load.argtypes = [_vp, ctypes.c_size_t, _i32, ctypes.POINTER(_
 _lib.sparsert_plan_load.restype = ctypes.c_int
 _lib.sparsert_plan_destroy.argtypes = [_vp]
 _lib.sparsert_plan_destroy.restype = None
-_lib.sparsert_rms_norm.argtypes = [_vp] * 8
+_lib.sparsert_rms_norm_workspace.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.sparsert_rms_norm_workspace.restype = ctypes.c_int
+_lib.sparsert_rms_norm.argtypes = [_vp] * 8 + [ctypes.c_size_t, _vp]
 _lib.sparsert_rms_norm.restype = ctypes.c_int
 _lib.sparsert_dequantize.argtypes = [_vp] * 6
 _lib.sparsert_dequantize.restype = ctypes.c_int
@@ -311,6 +313,12 @@ class RmsNorm(_Descriptor):
                  ldx: int = 0, ldh: int = 0, ldy: int = 0):
         super().__init__(_Norm(K, N, batch, dtype, dtype if out_dtype is None else out_dtype, ldx, ldh, ldy, eps))
 
+    def workspace_bytes(self) -> int:
+        """Device memory that a call can use (0 = none); calls that may run at the same time need it each."""
+        need = ctypes.c_size_t(0)
+        _check(_lib.sparsert_rms_norm_workspace(self.handle, ctypes.byref(need)))
+        return need.value
+
 
 class Dequantize(_Descriptor):
     """sparsert_dequant: the sizes, type and pitches of a dequantize call."""
@@ -333,9 +341,10 @@ class Adapters(_Descriptor):
         return need.value
 
 
-def rms_norm(norm: RmsNorm, X_dev: int, R_dev: int, gamma_dev: int, H_dev: int, Y_dev: int, scale_dev: int = 0, stream: int = 0):
-    """sparsert_rms_norm: Y = norm(X + R) * gamma, H = X + R; R, gamma and H may be 0 (none); scale for an int8 Y only."""
-    _check(_lib.sparsert_rms_norm(norm.handle, X_dev, R_dev, gamma_dev, H_dev, Y_dev, scale_dev, stream))
+def rms_norm(norm: RmsNorm, X_dev: int, R_dev: int, gamma_dev: int, H_dev: int, Y_dev: int, scale_dev: int = 0,
+             workspace_dev: int = 0, workspace_bytes: int = 0, stream: int = 0):
+    """sparsert_rms_norm: Y = norm(X + R) * gamma, H = X + R; R, gamma, H and the workspace may be 0 (none); scale for an int8 Y only."""
+    _check(_lib.sparsert_rms_norm(norm.handle, X_dev, R_dev, gamma_dev, H_dev, Y_dev, scale_dev, workspace_dev, workspace_bytes, stream))
 
 
 def dequantize(dequant: Dequantize, C_dev: int, row_scale_dev: int, col_scale_dev: int, Y_dev: int, stream: int = 0):

@@ -58,7 +58,26 @@ def norm_case(rng, K, N, dtype, batch=1, residual=True, gamma=True):
     return x, r, g
 
 
-def run_norm(x, r, g, out, eps=1e-5, pads=(0, 0, 0), keep=True, inplace=""):
+class Scratch:
+    """A workspace of NaN, with 64 bytes behind it that are not its own."""
+
+    def __init__(self, need):
+        self.need, self.t = need, torch.full((need + 64,), 255, dtype=torch.uint8, device=DEV)
+
+    def args(self):
+        return (self.t.data_ptr(), self.need) if self.need else (0, 0)
+
+    def check(self):
+        assert (self.t[self.need:].cpu().numpy() == 255).all()
+
+
+@pytest.fixture(params=["one kernel", "workspace"])
+def way(request):
+    """Norms without a workspace, and with one, which splits long columns over two kernels."""
+    return request.param == "workspace"
+
+
+def run_norm(way, x, r, g, out, eps=1e-5, pads=(0, 0, 0), keep=True, inplace=""):
     """Returns (y, scale, h).  pads: of X, of R and H, of Y.  inplace: "h=r", "h=x", "y=x", "y=r" in any combination."""
     b, K, N = x.shape
     X = Wide(x.shape, N + pads[0], x.dtype, x)
@@ -68,8 +87,10 @@ def run_norm(x, r, g, out, eps=1e-5, pads=(0, 0, 0), keep=True, inplace=""):
     scale = torch.full((b, N), -7.0, device=DEV) if np.dtype(out) == np.int8 else None
     G = vector(g) if g is not None else None
     d = sp.RmsNorm(K, N, dtype=KIND[x.dtype], out_dtype=KIND[np.dtype(out)], eps=eps, batch=b, ldx=N + pads[0], ldh=N + pads[1], ldy=N + pads[2])
-    sp.rms_norm(d, X.at, R.at if R else 0, at(G), H.at if H else 0, Y.at, at(scale), stream())
+    ws = Scratch(d.workspace_bytes())
+    sp.rms_norm(d, X.at, R.at if R else 0, at(G), H.at if H else 0, Y.at, at(scale), *(ws.args() if way else (0, 0)), stream())
     torch.cuda.synchronize()
+    ws.check()
     if not inplace:
         assert X.t.cpu().numpy().tobytes() == X.before.tobytes()
     return Y.read(), None if scale is None else scale.cpu().numpy(), H.read() if H else None
@@ -78,58 +99,58 @@ def run_norm(x, r, g, out, eps=1e-5, pads=(0, 0, 0), keep=True, inplace=""):
 @pytest.mark.parametrize("out", ["same", "int8"])
 @pytest.mark.parametrize("dtype", [np.float32, np.float16])
 @pytest.mark.parametrize("N", [1, 2, 3, 7, 8, 9, 16, 31, 33, 64, 65, 130, 517])
-def test_norm_at_the_edges_of_its_strips(N, dtype, out):
+def test_norm_at_the_edges_of_its_strips(N, dtype, out, way):
     rng = np.random.default_rng(N)
     for K in (1, 2, 63, 64, 65, 257, 1027):
         x, r, g = norm_case(rng, K, N, dtype, batch=1 if N > 100 else 2)
-        y, scale, h = run_norm(x, r, g, dtype if out == "same" else np.int8, pads=(0, 0, 0) if K % 2 else (5, 3, 9))
+        y, scale, h = run_norm(way, x, r, g, dtype if out == "same" else np.int8, pads=(0, 0, 0) if K % 2 else (5, 3, 9))
         plain.check_norm(y, scale, h, x, r, g, 1e-5)
 
 
 @pytest.mark.parametrize("out", ["same", "int8"])
 @pytest.mark.parametrize("dtype", [np.float32, np.float16])
 @pytest.mark.parametrize("K,N,batch", [(4096, 4, 1), (4096, 40, 1), (8192, 24, 1), (8200, 17, 2), (16385, 5, 1), (40000, 3, 1), (5000, 1030, 1), (130, 5003, 1)])
-def test_norm_of_long_columns_and_many_tokens(K, N, batch, dtype, out):
+def test_norm_of_long_columns_and_many_tokens(K, N, batch, dtype, out, way):
     x, r, g = norm_case(np.random.default_rng(K), K, N, dtype, batch)
-    y, scale, h = run_norm(x, r, g, dtype if out == "same" else np.int8, pads=(8, 8, 8) if N % 8 == 0 else (0, 1, 2))
+    y, scale, h = run_norm(way, x, r, g, dtype if out == "same" else np.int8, pads=(8, 8, 8) if N % 8 == 0 else (0, 1, 2))
     plain.check_norm(y, scale, h, x, r, g, 1e-5)
 
 
 @pytest.mark.parametrize("out", ["same", "int8"])
 @pytest.mark.parametrize("residual,gamma,keep", [(False, True, False), (True, False, False), (False, False, True), (True, True, False), (False, True, True)])
-def test_norm_without_residual_weights_or_sum(residual, gamma, keep, out):
+def test_norm_without_residual_weights_or_sum(residual, gamma, keep, out, way):
     rng = np.random.default_rng(3)
     for dtype, K, N in ((np.float16, 300, 70), (np.float32, 9000, 20)):
         x, r, g = norm_case(rng, K, N, dtype, residual=residual, gamma=gamma)
-        y, scale, h = run_norm(x, r, g, dtype if out == "same" else np.int8, keep=keep)
+        y, scale, h = run_norm(way, x, r, g, dtype if out == "same" else np.int8, keep=keep)
         plain.check_norm(y, scale, h, x, r, g, 1e-5)
 
 
 @pytest.mark.parametrize("inplace", ["h=r", "h=x", "y=x", "y=r", "h=r y=x", "h=x y=r"])
 @pytest.mark.parametrize("K,N", [(200, 19), (1027, 96), (9001, 21)])
-def test_norm_in_place(K, N, inplace):
+def test_norm_in_place(K, N, inplace, way):
     rng = np.random.default_rng(K)
     for dtype in (np.float16, np.float32):
         x, r, g = norm_case(rng, K, N, dtype, batch=2)
-        y, _, h = run_norm(x, r, g, dtype, pads=(3, 3, 3), inplace=inplace)
+        y, _, h = run_norm(way, x, r, g, dtype, pads=(3, 3, 3), inplace=inplace)
         plain.check_norm(y, None, h, x, r, g, 1e-5)
 
 
 @pytest.mark.parametrize("K", [70, 2000, 9000])
-def test_norm_of_columns_with_zeros_infinities_and_undefined_values(K):
+def test_norm_of_columns_with_zeros_infinities_and_undefined_values(K, way):
     rng = np.random.default_rng(4)
     for dtype in (np.float16, np.float32):
         x, _, g = norm_case(rng, K, 24, dtype, residual=False)
         x[0, :, 3] = 0
         x[0, :, 4] = np.finfo(dtype).smallest_subnormal
         x[0, 5, 7], x[0, K - 1, 9], x[0, K // 2, 15] = np.inf, np.nan, -np.inf
-        y, _, _ = run_norm(x, None, g, dtype)
+        y, _, _ = run_norm(way, x, None, g, dtype)
         sound = [n for n in range(24) if n not in (7, 9, 15)]
         plain.check_norm(y[..., sound], None, None, x[..., sound], None, g, 1e-5)
         assert np.isnan(y[0, :, 9]).all() and np.isnan(y[0, 5, 7]) and np.isnan(y[0, K // 2, 15])
         others = np.delete(y[0, :, 7], 5)
         assert (others == 0).all()                 # 1 / infinity
-        q, scale, _ = run_norm(x, None, g, np.int8)
+        q, scale, _ = run_norm(way, x, None, g, np.int8)
         plain.check_norm(q[..., sound], scale[..., sound], None, x[..., sound], None, g, 1e-5)
         assert (q[0, :, 3] == 0).all() and scale[0, 3] == 0
         for n in (7, 9, 15):
@@ -137,18 +158,18 @@ def test_norm_of_columns_with_zeros_infinities_and_undefined_values(K):
     x = np.full((1, 90, 9), 1e-3, dtype=np.float32)
     g = np.ones(90, dtype=np.float32)
     x[0, 4, 2], g[8] = 1e25, np.nan                # squares beyond binary32; an undefined weight
-    q, scale, _ = run_norm(x, None, g, np.int8)
+    q, scale, _ = run_norm(way, x, None, g, np.int8)
     assert (q == 0).all() and np.isnan(scale).all()
     g[8] = 1.0
-    q, scale, _ = run_norm(x, None, g, np.int8)
+    q, scale, _ = run_norm(way, x, None, g, np.int8)
     assert np.isnan(scale[0, 2]) and (q[0, :, 2] == 0).all() and np.isfinite(np.delete(scale[0], 2)).all()
 
 
-def test_norm_ties_go_to_the_even_integer():
+def test_norm_ties_go_to_the_even_integer(way):
     v = np.zeros((1, 8, 4), dtype=np.float32)
     v[0, :, 0] = [127, 0.5, 1.5, 2.5, -0.5, -1.5, -2.5, 126.5]
     v[0, :, 1] = -v[0, :, 0]
-    q, scale, _ = run_norm(v, None, None, np.int8)
+    q, scale, _ = run_norm(way, v, None, None, np.int8)
     assert q[0, :, 0].tolist() == [127, 0, 2, 2, 0, -2, -2, 126] and q[0, :, 1].tolist() == [-127, 0, -2, -2, 0, 2, 2, -126]
 
 
@@ -358,10 +379,11 @@ def chain(N, seed, batch=1, K=256, M=320):
     a = AdaptersCall(s)
     D = torch.zeros((batch, M, N), device=DEV)
     d, dq = sp.RmsNorm(K, N, dtype=sp.F16, out_dtype=sp.I8, eps=1e-5, batch=batch), sp.Dequantize(M, N, batch=batch)
+    nws = Scratch(d.workspace_bytes())
 
     def launch():
         st, v = stream(), a.v
-        sp.rms_norm(d, X.at, R.at, at(G), H.at, Q.at, at(scale), st)
+        sp.rms_norm(d, X.at, R.at, at(G), H.at, Q.at, at(scale), *nws.args(), st)
         sp.spmm(plan, Q.at, C.data_ptr(), st)
         sp.dequantize(dq, C.data_ptr(), at(v["row"]), at(scale), D.data_ptr(), st)
         sp.adapters(a.d, Q.at, at(v["down"]), at(v["up"]), at(v["index"]), at(v["alpha"]), C.data_ptr(), at(v["row"]), at(scale), a.Y.at, a.ws.data_ptr(), a.need, st)
@@ -379,6 +401,7 @@ def chain(N, seed, batch=1, K=256, M=320):
         for t in (H.t, Q.t, scale, C, D, a.Y.t):
             t.zero_()
         a.ws[:a.need] = 255
+        nws.t.fill_(255)
 
     launch.keep = plan
     return launch, check, clear
@@ -438,8 +461,10 @@ def test_problems_whose_offsets_pass_32_bits():
     X[..., :N], H[..., :N] = torch.from_numpy(x).to(DEV), torch.from_numpy(r).to(DEV)
     G, scale = vector(g), torch.zeros((batch, N), device=DEV)
     d = sp.RmsNorm(K, N, dtype=sp.F16, out_dtype=sp.I8, eps=1e-5, batch=batch, ldx=ld, ldh=ld, ldy=ld)
-    sp.rms_norm(d, X.data_ptr(), H.data_ptr(), at(G), H.data_ptr(), Q.data_ptr(), at(scale), stream())
+    nws = Scratch(d.workspace_bytes())
+    sp.rms_norm(d, X.data_ptr(), H.data_ptr(), at(G), H.data_ptr(), Q.data_ptr(), at(scale), *nws.args(), stream())
     torch.cuda.synchronize()
+    nws.check()
     q, sc = Q[..., :N].cpu().numpy(), scale.cpu().numpy()
     plain.check_norm(q, sc, H[..., :N].cpu().numpy(), x, r, g, 1e-5)
     del H

@@ -50,6 +50,7 @@ def norm(**kw):
     (dict(K=1 << 20, ldx=1 << 10), sp.EUNSUPPORTED, "2 GiB"), (dict(K=2 ** 31 - 1, N=2 ** 31 - 1), sp.EUNSUPPORTED, "2 GiB")])
 def test_norm_descriptors_that_are_refused(kw, status, text):
     refused(status, text, sp.rms_norm, norm(**kw), P, 0, 0, 0, Q)
+    refused(status, text, norm(**kw).workspace_bytes)
 
 
 def test_norm_calls_that_are_refused():
@@ -68,7 +69,15 @@ def test_norm_calls_that_are_refused():
     reserved = norm()
     reserved.fields.reserved[1] = 1
     refused(sp.EINVAL, "reserved", sp.rms_norm, reserved, P, 0, 0, 0, Q)
-    assert sp.raw.sparsert_rms_norm(None, P, None, None, None, Q, None, None) == sp.EINVAL
+    assert sp.raw.sparsert_rms_norm(None, P, None, None, None, Q, None, None, 0, None) == sp.EINVAL
+    size = ctypes.c_size_t()
+    assert sp.raw.sparsert_rms_norm_workspace(None, ctypes.byref(size)) == sp.EINVAL
+    assert sp.raw.sparsert_rms_norm_workspace(norm().handle, None) == sp.EINVAL
+    split = norm(K=8192, N=64)
+    need = split.workspace_bytes()
+    assert need > 0
+    refused(sp.EINVAL, "smaller", sp.rms_norm, split, P, 0, 0, 0, Q, 0, T, need - 1)
+    refused(sp.EINVAL, "16-byte", sp.rms_norm, split, P, 0, 0, 0, Q, 0, T + 4, need)
 
 
 @pytest.mark.parametrize("kw,status,text", [
