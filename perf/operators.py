@@ -179,6 +179,7 @@ def prepare(case, seed):
         s["sp"], s["stream"] = sp, torch.cuda.current_stream().cuda_stream
         if case["op"] == "norm":
             s["call"] = sp.RmsNorm(case["K"], N, dtype=kind[case["dtype"]], out_dtype=kind[case["out"]], eps=_EPS, batch=b, ldx=ld, ldh=ld, ldy=ld)
+            s["workspace"] = torch.empty(s["call"].workspace_bytes(), dtype=torch.uint8, device="cuda")
         elif case["op"] == "dequantize":
             s["call"] = sp.Dequantize(case["M"], N, dtype=kind[case["out"]], batch=b, ldc=ld, ldy=ld)
         else:
@@ -191,7 +192,8 @@ def prepare(case, seed):
 
 def _own_norm(s):
     at, N = s["at"], s["case"]["N"]
-    s["sp"].rms_norm(s["call"], at["x"], at["residual"], at["gamma"], at["h"], at["y"], at["scale"] if s["values"] is not None else 0, s["stream"])
+    s["sp"].rms_norm(s["call"], at["x"], at["residual"], at["gamma"], at["h"], at["y"], at["scale"] if s["values"] is not None else 0,
+                     at["workspace"], s["workspace"].numel(), s["stream"])
     if s["values"] is None:
         return {"sum": s["h"][..., :N], "out": s["y"][..., :N]}
     torch.mul(s["y"][..., :N], s["scale"][:, None, :], out=s["values"])   # what the int8 result stands for
