@@ -9,10 +9,10 @@
 namespace sparsert {
 
 template <typename Args>
-int launch_operator(const void *kernel, dim3 grid, int threads, Args &args, void *stream, std::string &err) {
+int launch_operator(const void *kernel, dim3 grid, int threads, Args &args, void *stream, std::string &err, int lds_bytes = 0) {
     static_assert(sizeof(Args) <= kArgBytes, "a longer argument block costs the host more per launch");
     void *list[] = {&args};
-    const hipError_t e = hipLaunchKernel(kernel, grid, dim3(threads), list, 0, static_cast<hipStream_t>(stream));
+    const hipError_t e = hipLaunchKernel(kernel, grid, dim3(threads), list, (size_t)lds_bytes, static_cast<hipStream_t>(stream));
     if (e == hipSuccess) return SPARSERT_OK;
     err = std::string("hipLaunchKernel: ") + hipGetErrorString(e);
     return SPARSERT_EHIP;
