@@ -341,23 +341,30 @@ class Adapters(_Descriptor):
         return need.value
 
 
-def rms_norm(norm: RmsNorm, X_dev: int, R_dev: int, gamma_dev: int, H_dev: int, Y_dev: int, scale_dev: int = 0,
+def _rms_norm(norm: RmsNorm, X_dev: int, R_dev: int, gamma_dev: int, H_dev: int, Y_dev: int, scale_dev: int = 0,
              workspace_dev: int = 0, workspace_bytes: int = 0, stream: int = 0):
     """sparsert_rms_norm: Y = norm(X + R) * gamma, H = X + R; R, gamma, H and the workspace may be 0 (none); scale for an int8 Y only."""
     _check(_lib.sparsert_rms_norm(norm.handle, X_dev, R_dev, gamma_dev, H_dev, Y_dev, scale_dev, workspace_dev, workspace_bytes, stream))
 
 
-def dequantize(dequant: Dequantize, C_dev: int, row_scale_dev: int, col_scale_dev: int, Y_dev: int, stream: int = 0):
+def _dequantize(dequant: Dequantize, C_dev: int, row_scale_dev: int, col_scale_dev: int, Y_dev: int, stream: int = 0):
     """sparsert_dequantize: Y = C * col_scale * row_scale; either scale may be 0 (ones)."""
     _check(_lib.sparsert_dequantize(dequant.handle, C_dev, row_scale_dev, col_scale_dev, Y_dev, stream))
 
 
-def adapters(adapter_set: Adapters, X_dev: int, down_dev: int, up_dev: int, index_dev: int, alpha_dev: int, C_dev: int,
+def _adapters(adapter_set: Adapters, X_dev: int, down_dev: int, up_dev: int, index_dev: int, alpha_dev: int, C_dev: int,
              row_scale_dev: int, col_scale_dev: int, Y_dev: int, workspace_dev: int, workspace_bytes: int, stream: int = 0):
     """sparsert_adapters: Y = C + alpha up (down x) of every token's adapter; alpha and, for int8 X, the scales may be 0 (ones)."""
     _check(_lib.sparsert_adapters(adapter_set.handle, X_dev, down_dev, up_dev, index_dev, alpha_dev, C_dev, row_scale_dev, col_scale_dev,
                                   Y_dev, workspace_dev, workspace_bytes, stream))
 
+
+if _fastcall is not None:
+    _fastcall.bind_operators(tuple(ctypes.cast(f, _vp).value for f in (_lib.sparsert_rms_norm, _lib.sparsert_dequantize, _lib.sparsert_adapters)),
+                             (_rms_norm, _dequantize, _adapters))
+    rms_norm, dequantize, adapters = _fastcall.rms_norm, _fastcall.dequantize, _fastcall.adapters
+else:
+    rms_norm, dequantize, adapters = _rms_norm, _dequantize, _adapters
 
 # Raw entry points for callers that time launches without Python argument handling.
 raw = _lib

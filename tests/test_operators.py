@@ -152,3 +152,61 @@ def test_wide_stores_have_no_scalar_offset(source, tmp_path):
     subprocess.run(flags + ["--offload-device-only", "-S", os.path.join(entry.CSRC, source)], check=True, capture_output=True)
     for store in re.findall(r"^\s+buffer_store_dwordx[34] (.*)", (tmp_path / "kernels.s").read_text(), re.M):
         assert re.fullmatch(r"v\[\d+:\d+\], (v\d+|off), s\[\d+:\d+\], 0( .*)?", store.split(";")[0].strip()), store
+
+
+def _outcome(call, args, kw):
+    try:
+        return call(*args, **kw)
+    except Exception as e:
+        return type(e).__name__, re.sub(r"\b_(rms_norm|dequantize|adapters)", r"\1", str(e)), getattr(e, "status", None)
+
+
+@pytest.mark.parametrize("which", ["rms_norm", "dequantize", "adapters"])
+def test_operator_calls_take_the_same_arguments_as_ctypes_does(which):
+    """Every call ends in the library's argument checks: an address is null or off its alignment."""
+    fast, general = getattr(sp, which), getattr(sp, "_" + which)
+    made, words = {"rms_norm": (norm(), [P, 0, 0, 0, Q + 1, 0, 0, 0]), "dequantize": (sp.Dequantize(8, 16), [P, 0, 0, Q + 1]),
+                   "adapters": (adapter_set(), [P, P, P, P, 0, Q, 0, 0, S + 1, T, 1 << 20])}[which]
+
+    class Wide:
+        handle = ctypes.c_void_p(made.handle)
+
+    class Closed:
+        handle = None
+
+    forms = [((made, *words), {}), ((made, *words, 0), {}), ((made, *words, None), {}), ((made, *words, 7), {}), ((made, *words), {"stream": 0}),
+             ((made, None, *words[1:]), {}), ((Wide, *words), {}), ((Closed, *words), {}), ((made, ctypes.c_void_p(P), *words[1:]), {}),
+             ((made, *words[:-1], True), {}), ((made, -16, *words[1:]), {}), ((made, 2 ** 64 + 16, *words[1:]), {}), ((made, *words, "s"), {}), ((made, 1.5, *words[1:]), {}),
+             ((made, *words[:2]), {}), ((), {}), ((made, *words, 0, 0), {}), ((made, *words), {"streem": 0}), ((None, *words), {}), ((made.handle, *words), {})]
+    refused_ = 0
+    for args, kw in forms:
+        want = _outcome(general, args, kw)
+        assert _outcome(fast, args, kw) == want, (args, kw)
+        refused_ += want is not None and want[0] == "SparseRTError"
+    assert refused_ >= 10
+
+
+def test_operators_work_without_the_c_functions():
+    import subprocess
+    import sys
+    code = """
+import sys
+sys.modules["paper_2008_11849_amd._fastcall"] = None   # what an import finds that was not built
+from paper_2008_11849_amd import sparsert as sp
+assert sp.rms_norm is sp._rms_norm and sp.dequantize is sp._dequantize and sp.adapters is sp._adapters
+for call, made, args in ((sp.rms_norm, sp.RmsNorm(8, 16), (0, 0, 0, 0, 0)), (sp.dequantize, sp.Dequantize(8, 16), (0, 0, 0, 0)),
+                         (sp.adapters, sp.Adapters(8, 8, 16, 4, 2), (0,) * 11)):
+    try:
+        call(made, *args, stream=0)
+    except sp.SparseRTError as e:
+        assert e.status == sp.EINVAL
+    else:
+        raise SystemExit("not refused")
+"""
+    res = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, res.stderr[-2000:]
+
+
+@pytest.mark.skipif(sp._fastcall is None, reason="built without the Python headers")
+def test_the_operators_are_called_through_the_c_functions():
+    assert sp.rms_norm is sp._fastcall.rms_norm and sp.dequantize is sp._fastcall.dequantize and sp.adapters is sp._fastcall.adapters
