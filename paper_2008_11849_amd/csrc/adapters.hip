@@ -1,11 +1,11 @@
 // Low-rank adapters of many requests beside a projection that they share, in two kernels:
-//   shrink  t[n, j] = sum_k down[a][j, k] x[k, n]         for the adapter a of every token, over a part of the rows k
-//   expand  Y[m, n] = c[m, n] + alpha[a] sum_j up[a][m, j] t[n, j]
-// t lies in the caller's workspace, [batch * N][part][ranks, rounded up to 16], in binary32.
+//   shrink  t[n, j] = alpha[a] sum_k down[a][j, k] x[k, n]     for the adapter a of every token, over a part of the rows k
+//   expand  Y[m, n] = c[m, n] + sum_j up[a][m, j] t[n, j]
+// t lies in the caller's workspace, [batch * N][part][ranks, rounded up to 16], in binary32.  (The factors are in t, so that the second kernel
+// fetches everything but `up` without waiting for an index.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cstdlib>
 
 #include "launch.h"
 #include "operators.h"
@@ -17,34 +17,63 @@ namespace sparsert {
 struct ShrinkArgs {
     const void *X, *down;
     const int32_t *index;
+    const float *alpha, *col;
     float *t;
     int32_t K, N, ldx, rank, count;
-    int32_t parts, slots;   // parts of K; workgroups that share the adapters of a tile of tokens
+    int32_t parts, turns, slots;   // parts of K, turns of a part; workgroups that share the adapters of a tile of tokens
 };
 
 struct ExpandArgs {
     const void *C, *up;
     const int32_t *index;
-    const float *alpha, *row, *col, *t;
+    const float *row, *col, *t;
     void *Y;
     int32_t M, N, ldc, ldy, count, parts;
-    int32_t rows;          // of a workgroup,
-    int16_t tokens, rank;  // and its tokens
+    int32_t rows;          // of a workgroup
+    int32_t rank;
 };
 
 __device__ __forceinline__ int ranks16(int rank) { return (rank + 15) & ~15; }
 
-// V adjacent weights of a row from element `at` of it on: all in range if `whole`, else those before `end` and zeros.  (What lies behind a row is the
-// next one, and may be infinite: it has to be left out, not multiplied by zero.)
-template <typename W, int V> __device__ __forceinline__ void weights(const Matrix &m, uint32_t row_at, int at, int end, bool whole, W (&to)[V]) {
-    constexpr int PIECE = 16 / sizeof(W);
+// 16 bytes of weights of a row of `end` elements, from element `at` on; zeros for those behind the row's end.  (There lies the next row, which may hold
+// infinities: it has to be left out, not multiplied by zero.)  `whole`: no piece is cut short by the end.  A piece that is reads the row's last 16 bytes and moves
+// them down.  A row shorter than that is read over its end, so it has an even number of halves: a range is checked in steps of four bytes.
+template <typename W> struct Piece { W v[16 / sizeof(W)]; };
+template <typename W> __device__ __forceinline__ Piece<W> piece(const Matrix &m, uint32_t row_at, uint32_t common, int at, int end, bool whole) {
+    constexpr int LANE = 16 / sizeof(W), BITS = 8 * sizeof(W);
+    Piece<W> p;
     if (whole) {
+        load<W, LANE>(m, at < end ? row_at + (uint32_t)at * (uint32_t)sizeof(W) : kNowhere, common, p.v);
+        return p;
+    }
+    const int from = max(min(at, end - LANE), 0);
+    load<W, LANE>(m, at < end ? row_at + (uint32_t)from * (uint32_t)sizeof(W) : kNowhere, common, p.v);
+    uint64_t u[2];
+    __builtin_memcpy(u, p.v, 16);
+    const int down = (at - from) * BITS, keep = (end - at) * BITS;   // (of lanes behind the end: nothing is there)
+    if (end < LANE) {
+        u[1] &= keep > 64 ? ~0ull >> (128 - keep & 63) : 0;
+        u[0] &= keep >= 64 ? ~0ull : ~0ull >> (64 - keep & 63);
+    } else if (at < end) {
+        const uint64_t low = u[0], high = u[1];
+        u[0] = down == 0 ? low : down < 64 ? low >> (down & 63) | high << (64 - down & 63) : high >> (down - 64 & 63);
+        u[1] = down < 64 ? high >> (down & 63) : 0;
+    }
+    __builtin_memcpy(p.v, u, 16);
+    return p;
+}
+// Can rows of `end` elements be read so?
+template <typename W> bool pieces_fit(int end) { return end >= 16 / (int)sizeof(W) || end * sizeof(W) % 4 == 0; }
+
+// The same for V elements and rows of any length.
+template <typename W, int V> __device__ __forceinline__ void weights(const Matrix &m, uint32_t row_at, int at, int end, bool whole, W (&to)[V]) {
+    constexpr int LANE = 16 / sizeof(W);
+    if (whole || end >= LANE) {
 #pragma unroll
-        for (int p = 0; p < V / PIECE; ++p) {
-            W piece[PIECE];
-            load<W, PIECE>(m, row_at + (uint32_t)(at + p * PIECE) * (uint32_t)sizeof(W), 0, piece);
+        for (int p = 0; p < V / LANE; ++p) {
+            const Piece<W> q = piece<W>(m, row_at, 0, at + p * LANE, end, whole);
 #pragma unroll
-            for (int i = 0; i < PIECE; ++i) to[p * PIECE + i] = piece[i];
+            for (int i = 0; i < LANE; ++i) to[p * LANE + i] = q.v[i];
         }
     } else {
 #pragma unroll
@@ -61,12 +90,12 @@ template <typename W, int V> __device__ __forceinline__ void weights(const Matri
 constexpr int kTokenGroup = 8, kTokenRows = 512, kTokenThreads = 512;   // tokens and rows of x of a workgroup; a wave for each token
 
 // The group's x goes to LDS once, whole rows of eight tokens at a time (V = 8; 1: fewer than eight tokens); then wave w has token w, and its lane l the rows 8 l ... 8 l + 7,
-// which it multiplies with 16 rows of `down` at a time.
-template <typename X, typename W, int V> __global__ __launch_bounds__(kTokenThreads) void shrink_tokens_kernel(const ShrinkArgs a) {
+// which it multiplies with 16 rows of `down`; other workgroups have the others.
+template <typename X, typename W, int V, bool WHOLE> __global__ __launch_bounds__(kTokenThreads) void shrink_tokens_kernel(const ShrinkArgs a) {
     __shared__ __align__(16) float xs[kTokenGroup][kTokenRows + 4];
-    const int groups = (a.N + kTokenGroup - 1) / kTokenGroup;
-    if ((int)blockIdx.x >= groups * a.parts) return;
-    const int group = blockIdx.x % groups, part = blockIdx.x / groups, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int groups = (a.N + kTokenGroup - 1) / kTokenGroup, ranks = ranks16(a.rank), blocks = ranks / 16;
+    if ((int)blockIdx.x >= groups * a.parts * blocks) return;
+    const int group = blockIdx.x % groups, part = blockIdx.x / groups % a.parts, j0 = blockIdx.x / groups / a.parts * 16, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int n0 = group * kTokenGroup, k0 = part * kTokenRows, n = n0 + wave;
     const int id = n < a.N ? a.index[(size_t)blockIdx.y * a.N + n] : -1;
     {
@@ -96,49 +125,70 @@ template <typename X, typename W, int V> __global__ __launch_bounds__(kTokenThre
     float x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = xs[wave][lane * 8 + i];
-    const int ranks = ranks16(a.rank), k = k0 + lane * 8;
-    const bool whole = k0 + kTokenRows <= a.K || a.K % 8 == 0;   // no lane's eight rows end before it does
+    const int k = k0 + lane * 8;
     const Matrix down(static_cast<const W *>(a.down) + (size_t)id * a.rank * a.K, a.rank, a.K, a.K, sizeof(W));
-    float *const to = a.t + (((size_t)blockIdx.y * a.N + n) * a.parts + part) * ranks;
-    for (int j0 = 0; j0 < ranks; j0 += 16) {
-        W w[16][8];
-        float s[16];
+    const float alpha = a.alpha ? a.alpha[id] : 1.0f, col = a.col ? a.col[(size_t)blockIdx.y * a.N + n] : 1.0f;
+    W w[16][8];
+    float s[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) weights<W, 8>(down, j0 + j < a.rank && k < a.K ? (uint32_t)(j0 + j) * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, k, a.K, whole, w[j]);
+    for (int j = 0; j < 16; ++j) weights<W, 8>(down, j0 + j < a.rank && k < a.K ? (uint32_t)(j0 + j) * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, k, a.K, WHOLE || k0 + kTokenRows <= a.K, w[j]);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            s[j] = 0.0f;
+    for (int j = 0; j < 16; ++j) {
+        s[j] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[j] = __builtin_fmaf((float)w[j][i], x[i], s[j]);
-        }
-        float sum[1];
-        over_rows<16, 1, false>(s, lane, sum);
-        if (stores<16, 1>(lane)) to[j0 + column_of<16, 1>(lane)] = sum[0];
+        for (int i = 0; i < 8; ++i) s[j] = __builtin_fmaf((float)w[j][i], x[i], s[j]);
     }
+    float sum[1];
+    over_rows<16, 1, false>(s, lane, sum);
+    if (stores<16, 1>(lane)) a.t[(((size_t)blockIdx.y * a.N + n) * a.parts + part) * ranks + j0 + column_of<16, 1>(lane)] = sum[0] * alpha * col;
 }
 
-// t of `tokens` tokens from n0 on, its parts added up in order, times everything that does not depend on the row, to LDS; zeros for tokens without adapter.
-template <bool SCALED> __device__ __forceinline__ void gather_t(const ExpandArgs &a, int n0, int tokens, int threads, float *ts, int pitch) {
-    const int ranks = ranks16(a.rank);
-    for (int i = threadIdx.x; i < tokens * ranks; i += threads) {
-        const int c = i / ranks, j = i - c * ranks, n = n0 + c;
-        float s = 0.0f;
-        const int id = n < a.N ? a.index[(size_t)blockIdx.y * a.N + n] : -1;
-        if (id >= 0 && id < a.count) {
-            const float *from = a.t + ((size_t)blockIdx.y * a.N + n) * a.parts * ranks + j;
-            for (int p0 = 0; p0 < a.parts; p0 += 8) {
-                float u[8];
+// t of up to TOKENS tokens from n0 on to LDS, rows of `pitch`: the parts added up in order.  THREADS / TOKENS threads share a token, each of them with four adjacent
+// ranks at a time, RANKS ranks in a turn.  Tokens without adapter get what happens to lie there.  Returns the largest |t| of this thread's.
+template <int THREADS, int RANKS, int TOKENS = 64> struct GatherT {
+    static constexpr int SHARE = THREADS / TOKENS, AT_ONCE = 4, OWN = RANKS / (SHARE * 4);
+    static_assert(RANKS % (SHARE * 4) == 0 && OWN >= 1, "whole turns");
+    const float4 *from;
+    float4 u[AT_ONCE][OWN];
+    int parts, ranks, c, share;
+    bool mine;
+    __device__ __forceinline__ void fetch(int j0, int p0) {
 #pragma unroll
-                for (int p = 0; p < 8; ++p) u[p] = p0 + p < a.parts ? from[(size_t)(p0 + p) * ranks] : 0.0f;
+        for (int p = 0; p < AT_ONCE; ++p)
 #pragma unroll
-                for (int p = 0; p < 8; ++p) s += u[p];
+            for (int i = 0; i < OWN; ++i) {
+                const int j = j0 + (share + i * SHARE) * 4;
+                u[p][i] = mine && p0 + p < parts && j < ranks ? from[((p0 + p) * ranks + j) / 4] : float4{0.0f, 0.0f, 0.0f, 0.0f};
             }
-            if (a.alpha) s *= a.alpha[id];
-            if (SCALED && a.col) s *= a.col[(size_t)blockIdx.y * a.N + n];
-        }
-        ts[c * pitch + j] = s;
     }
-}
+    // Sends for the first of it.
+    __device__ __forceinline__ GatherT(const ExpandArgs &a, int n0, int tokens) : parts(a.parts), ranks(ranks16(a.rank)), c((int)threadIdx.x / SHARE), share((int)threadIdx.x % SHARE), mine(c < tokens) {
+        from = reinterpret_cast<const float4 *>(a.t + ((size_t)blockIdx.y * a.N + n0 + c) * parts * ranks);
+        fetch(0, 0);
+    }
+    __device__ __forceinline__ float finish(float *ts, int pitch, int row) {   // row: of this thread's token
+        float top = 0.0f;
+        for (int j0 = 0; j0 < ranks; j0 += RANKS) {
+            float4 s[OWN];
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) s[i] = float4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int p0 = 0; p0 < parts; p0 += AT_ONCE) {
+                if (j0 > 0 || p0 > 0) fetch(j0, p0);
+#pragma unroll
+                for (int p = 0; p < AT_ONCE; ++p)
+#pragma unroll
+                    for (int i = 0; i < OWN; ++i) s[i].x += u[p][i].x, s[i].y += u[p][i].y, s[i].z += u[p][i].z, s[i].w += u[p][i].w;
+            }
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) {
+                const int j = j0 + (share + i * SHARE) * 4;
+                if (mine && j < ranks) *reinterpret_cast<float4 *>(ts + row * pitch + j) = s[i];
+                top = larger(larger(larger(fabsf(s[i].x), fabsf(s[i].y)), larger(fabsf(s[i].z), fabsf(s[i].w))), top);
+            }
+        }
+        return top;
+    }
+};
 
 // Y of V tokens of a row: the projection's result, scaled, and what the adapter adds.
 template <typename C, typename W, int V> __device__ __forceinline__ void finish(const float (&c)[V], const float (&col)[V], float row, const float (&add)[V], W (&y)[V]) {
@@ -146,51 +196,76 @@ template <typename C, typename W, int V> __device__ __forceinline__ void finish(
     for (int v = 0; v < V; ++v) y[v] = (W)((std::is_same<C, int32_t>::value ? c[v] * col[v] * row : c[v]) + add[v]);
 }
 
-// A workgroup does 64 rows of Y for up to 64 tokens: a wave takes a token, its lane l row l; the sums meet the rows of C through LDS, so that both are read and written along the rows.
-constexpr int kExpandTokens = 64, kExpandRows = 64, kExpandThreads = 1024;
+// A workgroup does 64 rows of Y for 16 * EACH tokens: a wave takes EACH of them, its lane l row l; the sums meet the rows of C through LDS, so that both are read and written along the rows.
+constexpr int kExpandRows = 64, kExpandThreads = 1024, kExpandWaves = kExpandThreads / 64;
 
-template <typename C, typename W> __global__ __launch_bounds__(kExpandThreads) void expand_tokens_kernel(const ExpandArgs a) {
+template <typename C, typename W, int EACH, bool WHOLE> __global__ __launch_bounds__(kExpandThreads) void expand_tokens_kernel(const ExpandArgs a) {
+    constexpr int TOKENS = EACH * kExpandWaves;
     constexpr bool SCALED = std::is_same<C, int32_t>::value;
-    extern __shared__ __align__(16) float lds[];
-    float *const ys = lds;                                                  // [row][token], rows 65 apart
+    extern __shared__ __align__(16) float ts[];           // [token][rank]
+    __shared__ float ys[kExpandRows * (TOKENS + 1)];      // [row][token]
     const int ranks = ranks16(a.rank);
-    float *const ts = lds + kExpandRows * (kExpandTokens + 1) + 16 - (kExpandRows * (kExpandTokens + 1)) % 16;   // [token][rank]
-    const int blocks = (a.M + kExpandRows - 1) / kExpandRows, m0 = (int)(blockIdx.x % blocks) * kExpandRows, n0 = (int)(blockIdx.x / blocks) * a.tokens;
+    const int blocks = (a.M + kExpandRows - 1) / kExpandRows, m0 = (int)(blockIdx.x % blocks) * kExpandRows, n0 = (int)(blockIdx.x / blocks) * TOKENS;
     if (n0 >= a.N) return;
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), tokens = min(a.tokens, a.N - n0);
-    gather_t<SCALED>(a, n0, tokens, kExpandThreads, ts, ranks);
-    __syncthreads();
-    for (int c = wave; c < tokens; c += kExpandThreads / 64) {
-        const int id = __builtin_amdgcn_readfirstlane(a.index[(size_t)blockIdx.y * a.N + n0 + c]);
-        float s = -0.0f;   // (what is added to nothing leaves it as it is)
-        if (id >= 0 && id < a.count) {
-            const Matrix up(static_cast<const W *>(a.up) + (size_t)id * a.M * a.rank, a.M, a.rank, a.rank, sizeof(W));
-            const uint32_t row_at = m0 + lane < a.M ? (uint32_t)(m0 + lane) * (uint32_t)a.rank * (uint32_t)sizeof(W) : kNowhere;
-            s = 0.0f;
-            for (int j0 = 0; j0 < a.rank; j0 += 16) {
-                W u[2][8];
-                weights<W, 8>(up, row_at, j0, a.rank, j0 + 8 <= a.rank, u[0]);
-                weights<W, 8>(up, row_at, j0 + 8, a.rank, j0 + 16 <= a.rank, u[1]);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s = __builtin_fmaf((float)u[i / 8][i % 8], ts[c * ranks + j0 + i], s);
-            }
-        }
-        ys[lane * (kExpandTokens + 1) + c] = s;
-    }
-    __syncthreads();
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), tokens = min(TOKENS, a.N - n0);
+    // Everything that waits for nothing is on its way first: this thread's elements of C, the indices of its wave's tokens, t.
+    constexpr int OWN = kExpandRows * TOKENS / kExpandThreads;   // elements of a thread
     const Matrix from(static_cast<const C *>(a.C) + (int64_t)blockIdx.y * a.M * a.ldc, a.M, a.N, a.ldc, sizeof(C));
-    const Matrix Y(static_cast<W *>(a.Y) + (int64_t)blockIdx.y * a.M * a.ldy, a.M, a.N, a.ldy, sizeof(W));
-    for (int i = t; i < kExpandRows * tokens; i += kExpandThreads) {
-        const int r = i / tokens, c = i - r * tokens, m = m0 + r;
-        if (m >= a.M) continue;
-        C had[1];
-        load<C, 1>(from, ((uint32_t)m * (uint32_t)a.ldc + (uint32_t)(n0 + c)) * (uint32_t)sizeof(C), 0, had);
-        const float c1[1] = {(float)had[0]}, col[1] = {SCALED && a.col ? a.col[(size_t)blockIdx.y * a.N + n0 + c] : 1.0f};
-        const float add[1] = {ys[r * (kExpandTokens + 1) + c]};
-        W y[1];
-        finish<C, W, 1>(c1, col, SCALED && a.row ? a.row[m] : 1.0f, add, y);
-        store<W, 1>(Y, ((uint32_t)m * (uint32_t)a.ldy + (uint32_t)(n0 + c)) * (uint32_t)sizeof(W), 0, 0, y);
+    C had[OWN];
+    int row[OWN], token[OWN], id[EACH];
+#pragma unroll
+    for (int q = 0; q < EACH; ++q) id[q] = wave + q * kExpandWaves < tokens ? a.index[(size_t)blockIdx.y * a.N + n0 + wave + q * kExpandWaves] : -1;
+    constexpr int TURN = 4 * kExpandThreads / TOKENS;   // ranks
+    GatherT<kExpandThreads, TURN, TOKENS> gather(a, n0, tokens);
+#pragma unroll
+    for (int o = 0; o < OWN; ++o) {
+        const int i = t + o * kExpandThreads;
+        row[o] = i / tokens;
+        token[o] = i - row[o] * tokens;
+        C one[1];
+        load<C, 1>(from, row[o] < kExpandRows && m0 + row[o] < a.M ? ((uint32_t)(m0 + row[o]) * (uint32_t)a.ldc + (uint32_t)(n0 + token[o])) * (uint32_t)sizeof(C) : kNowhere, 0, one);
+        had[o] = one[0];
     }
+    float s[EACH];
+#pragma unroll
+    for (int q = 0; q < EACH; ++q) {
+        id[q] = __builtin_amdgcn_readfirstlane(id[q]);
+        if (id[q] >= a.count) id[q] = -1;
+        s[q] = id[q] >= 0 ? 0.0f : -0.0f;   // (what is added to nothing leaves it as it is)
+    }
+    for (int j0 = 0; j0 < a.rank; j0 += 16) {
+        W u[EACH][2][8];
+#pragma unroll
+        for (int q = 0; q < EACH; ++q)
+            if (id[q] >= 0) {
+                const Matrix up(static_cast<const W *>(a.up) + (size_t)id[q] * a.M * a.rank, a.M, a.rank, a.rank, sizeof(W));
+                const uint32_t row_at = m0 + lane < a.M ? (uint32_t)(m0 + lane) * (uint32_t)a.rank * (uint32_t)sizeof(W) : kNowhere;
+                weights<W, 8>(up, row_at, j0, a.rank, WHOLE, u[q][0]);
+                weights<W, 8>(up, row_at, j0 + 8, a.rank, WHOLE, u[q][1]);
+            }
+        if (j0 == 0) {
+            gather.finish(ts, ranks, gather.c);
+            __syncthreads();
+        }
+#pragma unroll
+        for (int q = 0; q < EACH; ++q)
+            if (id[q] >= 0)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[q] = __builtin_fmaf((float)u[q][i / 8][i % 8], ts[(wave + q * kExpandWaves) * ranks + j0 + i], s[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < EACH; ++q) ys[lane * (TOKENS + 1) + wave + q * kExpandWaves] = s[q];
+    __syncthreads();
+    const Matrix Y(static_cast<W *>(a.Y) + (int64_t)blockIdx.y * a.M * a.ldy, a.M, a.N, a.ldy, sizeof(W));
+#pragma unroll
+    for (int o = 0; o < OWN; ++o)
+        if (row[o] < kExpandRows && m0 + row[o] < a.M) {
+            const float c1[1] = {(float)had[o]}, col[1] = {SCALED && a.col ? a.col[(size_t)blockIdx.y * a.N + n0 + token[o]] : 1.0f};
+            const float add[1] = {ys[row[o] * (TOKENS + 1) + token[o]]};
+            W y[1];
+            finish<C, W, 1>(c1, col, SCALED && a.row ? a.row[m0 + row[o]] : 1.0f, add, y);
+            store<W, 1>(Y, ((uint32_t)(m0 + row[o]) * (uint32_t)a.ldy + (uint32_t)(n0 + token[o])) * (uint32_t)sizeof(W), 0, 0, y);
+        }
 }
 
 // ---- Many tokens: tiles of 64 on the matrix cores.
@@ -209,18 +284,18 @@ struct TileTokens {
     Columns<4> columns;
     int id[4];
     __device__ __forceinline__ TileTokens(const int32_t *index, int count, int n0, int N, int lane) : columns(n0 + (lane & 15) * 4, N) {
+        const Matrix m(index + (size_t)blockIdx.y * N, 1, N, N, 4);
+        load<int32_t, 4>(m, columns.any ? (uint32_t)columns.first * 4u : kNowhere, 0, id);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            id[c] = columns.any && c >= columns.skip ? index[(size_t)blockIdx.y * N + columns.first + c] : -1;
-            if (id[c] >= count) id[c] = -1;
-        }
+        for (int c = 0; c < 4; ++c)
+            if (!columns.any || c < columns.skip || (uint32_t)id[c] >= (uint32_t)count) id[c] = -1;
     }
     // The adapters of the tile one after the other, each once: the next one, with its tokens taken out of `left`, or -1.  Uniform.
     static __device__ __forceinline__ int next(int (&left)[4]) {
-        int a = -1;
-#pragma unroll
-        for (int c = 3; c >= 0; --c)
-            if (const uint64_t have = __ballot(left[c] >= 0)) a = __builtin_amdgcn_readlane(left[c], __builtin_ctzll(have));
+        const uint32_t any = min(min((uint32_t)left[0], (uint32_t)left[1]), min((uint32_t)left[2], (uint32_t)left[3]));   // (-1 is the largest)
+        const uint64_t lanes = __ballot(any != 0xffffffffu);
+        if (lanes == 0) return -1;
+        const int a = __builtin_amdgcn_readlane((int)any, __builtin_ctzll(lanes));
 #pragma unroll
         for (int c = 0; c < 4; ++c)
             if (left[c] == a) left[c] = -1;
@@ -248,222 +323,328 @@ template <> struct Step<float> {
 
 constexpr int kShrinkWaves = 8;
 
-// A workgroup does 64 tokens and a part of 8 * STEPS steps of K: wave w keeps its STEPS steps of x in registers and multiplies them with 16 ranks of an
-// adapter at a time; the waves' sums meet in LDS.
-template <typename X, typename W, int STEPS> __global__ __launch_bounds__(kShrinkWaves * 64, 2) void shrink_tiles_kernel(const ShrinkArgs a) {
+// A workgroup does 64 tokens and a part of K, its eight waves a step each at a time (256 rows of half weights, 128 of binary32); what a turn needs from
+// memory is fetched while the one before it is computed.  When an adapter's last turn is done, the waves' sums meet in LDS.
+template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds__(kShrinkWaves * 64, 2) void shrink_tiles_kernel(const ShrinkArgs a) {
     typedef Step<W> Q;
     typedef typename Q::frag frag;
-    constexpr int WAVE_ROWS = STEPS * Q::ROWS, PART = kShrinkWaves * WAVE_ROWS;
-    __shared__ __align__(16) float4v sums[2][kShrinkWaves][4][64];
+    constexpr int TURN = kShrinkWaves * Q::ROWS;
+    __shared__ __align__(16) float4v sums[RB][kShrinkWaves][4][64];
     __shared__ int ids[kTile];
     const int tiles = (a.N + kTile - 1) / kTile, task = task_of(blockIdx.x, tiles * a.parts * a.slots);
     if (task >= tiles * a.parts * a.slots) return;
     const int slot = task % a.slots, part = task / a.slots % a.parts, n0 = task / a.slots / a.parts * kTile;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, i = lane & 15;
     const TileTokens tokens(a.index, a.count, n0, a.N, lane);
+    const int ranks = ranks16(a.rank), first = part * a.turns, last = min(first + a.turns, (a.K + TURN - 1) / TURN);   // turns of this part
+    const Matrix from(static_cast<const X *>(a.X) + (int64_t)blockIdx.y * a.K * a.ldx, a.K, a.N, a.ldx, sizeof(X));
+    struct Loads { X v[Q::LANE][4]; frag w[RB]; };
+    Loads even, odd;
+    // Offsets of a lane in a turn.  Rows of x past K lie outside of it.  (What the lanes share, the turn's first row, does not: a range is checked
+    // after it has been taken off.)
+    const int lane_row = wave * Q::ROWS + g * Q::LANE;
+    uint32_t x_at[Q::LANE];
+#pragma unroll
+    for (int e = 0; e < Q::LANE; ++e)
+        x_at[e] = tokens.columns.any ? ((uint32_t)(lane_row + e) * (uint32_t)a.ldx + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(X) : kNowhere;
+    auto fetch_x = [&](int turn, Loads &l) {
+#pragma unroll
+        for (int e = 0; e < Q::LANE; ++e) load<X, 4>(from, x_at[e], (uint32_t)turn * (uint32_t)TURN * (uint32_t)a.ldx * (uint32_t)sizeof(X), l.v[e]);
+    };
+    auto fetch_w = [&](int id, int turn, Loads &l) {
+        const Matrix down(static_cast<const W *>(a.down) + (size_t)id * a.rank * a.K, a.rank, a.K, a.K, sizeof(W));
+        const int k = turn * TURN + lane_row;
+        if constexpr (WHOLE) {
+            const uint32_t at = k < a.K ? ((uint32_t)i * (uint32_t)a.K + (uint32_t)lane_row) * (uint32_t)sizeof(W) : kNowhere;   // (ranks past the last lie outside, too)
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                W v[Q::LANE];
+                load<W, Q::LANE>(down, at + (k < a.K ? (uint32_t)(b * 16) * (uint32_t)a.K * (uint32_t)sizeof(W) : 0), (uint32_t)turn * (uint32_t)TURN * (uint32_t)sizeof(W), v);
+                __builtin_memcpy(&l.w[b], v, 16);
+            }
+        } else {
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const Piece<W> p = piece<W>(down, b * 16 + i < a.rank ? (uint32_t)(b * 16 + i) * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, 0, k, a.K, false);
+                __builtin_memcpy(&l.w[b], p.v, 16);
+            }
+        }
+    };
+    fetch_x(first, even);
     int left[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) left[c] = tokens.id[c];
-    auto next = [&]() {   // of this workgroup's adapters: every slots-th, from the slot-th on
-        return TileTokens::next(left);
+    auto next = [&](int n) {   // the n-th adapter from here, or -1
+        int id;
+        do id = TileTokens::next(left);
+        while (id >= 0 && --n > 0);
+        return id;
     };
-    int id = -1;
-    for (int skip = slot; skip >= 0; --skip) {
-        id = next();
-        if (id < 0) return;
-    }
+    int id = next(slot + 1);   // of this workgroup's adapters: every slots-th, from the slot-th on
+    if (id < 0) return;
+    fetch_w(id, first, even);
     if (wave == 0 && g == 0)
 #pragma unroll
         for (int c = 0; c < 4; ++c) ids[i * 4 + c] = tokens.id[c];
-    const int k0 = part * PART + wave * WAVE_ROWS;
-    frag x[STEPS][4];
-    {
-        const Matrix from(static_cast<const X *>(a.X) + (int64_t)blockIdx.y * a.K * a.ldx, a.K, a.N, a.ldx, sizeof(X));
-        X v[STEPS][Q::LANE][4];
+    // Thread t: two ranks of a token, the waves' sums in their order.
+    const int item = t >> 1, of_c = item >> 6, of_lane = item & 63, n = min(n0 + (of_lane & 15) * 4, a.N - 4) + of_c;
+    float *const to = a.t + (((size_t)blockIdx.y * a.N + n) * a.parts + part) * ranks + (of_lane >> 4) * 4 + (t & 1) * 2;
+    const float col = a.col ? a.col[(size_t)blockIdx.y * a.N + n] : 1.0f;
+    float4v acc[RB][4];
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
+    for (int b = 0; b < RB; ++b)
 #pragma unroll
-            for (int e = 0; e < Q::LANE; ++e) {
-                const int k = k0 + s * Q::ROWS + g * Q::LANE + e;
-                load<X, 4>(from, k < a.K && tokens.columns.any ? ((uint32_t)k * (uint32_t)a.ldx + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(X) : kNowhere, 0, v[s][e]);
-            }
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s)
+        for (int c = 0; c < 4; ++c) acc[b][c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    frag x[4];
+    int turn = first, then = next(a.slots);   // then: the adapter after this one
+    bool fresh = true, met = false;           // is x of this turn still to be made; have sums met already?
+    // One turn; false when it was the last one.
+    auto step = [&](Loads &now, Loads &ahead) {
+        const bool done = turn + 1 == last;
+        if (!done) {
+            fetch_x(turn + 1, ahead);
+            fetch_w(id, turn + 1, ahead);
+        } else if (then >= 0) {
+            if (last - first > 1) fetch_x(first, ahead);
+            fetch_w(then, first, ahead);
+        }
+        if (fresh)
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int e = 0; e < Q::LANE; ++e) x[s][c][e] = (W)v[s][e][c];
-    }
-    const int ranks = ranks16(a.rank);
-    const bool whole = k0 + WAVE_ROWS <= a.K || a.K % Q::LANE == 0;   // no lane's rows end before they do
-    auto fetch = [&](int id, int j0, frag (&w)[STEPS]) {
-        const Matrix down(static_cast<const W *>(a.down) + (size_t)id * a.rank * a.K, a.rank, a.K, a.K, sizeof(W));
+                for (int e = 0; e < Q::LANE; ++e) x[c][e] = (W)now.v[e][c];
+        fresh = last - first > 1;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const int k = k0 + s * Q::ROWS + g * Q::LANE;
-            W v[Q::LANE];
-            weights<W, Q::LANE>(down, j0 + i < a.rank && k < a.K ? (uint32_t)(j0 + i) * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, k, a.K, whole, v);
+        for (int b = 0; b < RB; ++b)
 #pragma unroll
-            for (int e = 0; e < Q::LANE; ++e) w[s][e] = v[e];
+            for (int c = 0; c < 4; ++c) acc[b][c] = Q::mma(now.w[b], x[c], acc[b][c]);
+        if (!done) {
+            ++turn;
+            return true;
         }
-    };
-    frag w[STEPS];
-    fetch(id, 0, w);
-    for (int turn = 0, j0 = 0; id >= 0; ++turn) {
-        float4v acc[4];
+        const float alpha = a.alpha ? a.alpha[id] : 1.0f;
+        if (met) __syncthreads();   // the last adapter's sums have been read
+        met = true;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            acc[c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int b = 0; b < RB; ++b)
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) acc[c] = Q::mma(w[s], x[s][c], acc[c]);
-        }
-        const int of = id, at = j0;
-        j0 += 16;
-        if (j0 >= ranks) {
-            j0 = 0;
-            for (int skip = a.slots; skip > 0 && id >= 0; --skip) id = next();
-        }
-        if (id >= 0) fetch(id, j0, w);   // the next turn's weights are on their way while the sums meet
-        float4v(*const mine)[4][64] = sums[turn & 1];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) mine[wave][c][lane] = acc[c];
-        __syncthreads();   // (the buffer of the turn before last was read before the last turn's barrier)
-        // Thread t: two ranks of a token, the waves' sums in their order.
-        const int item = t >> 1, c = item >> 6, l = item & 63, n = min(n0 + (l & 15) * 4, a.N - 4) + c;
-        if (ids[(l & 15) * 4 + c] == of) {
-            float2 sum = {0.0f, 0.0f};
-#pragma unroll
-            for (int v = 0; v < kShrinkWaves; ++v) {
-                const float2 u = *(reinterpret_cast<const float2 *>(&mine[v][c][l]) + (t & 1));
-                sum.x += u.x;
-                sum.y += u.y;
+            for (int c = 0; c < 4; ++c) {
+                sums[b][wave][c][lane] = acc[b][c];
+                acc[b][c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
             }
-            float *const to = a.t + (((size_t)blockIdx.y * a.N + n) * a.parts + part) * ranks + at + (l >> 4) * 4 + (t & 1) * 2;
-            *reinterpret_cast<float2 *>(to) = sum;
+        __syncthreads();
+        if (ids[(of_lane & 15) * 4 + of_c] == id) {
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                float2 sum = {0.0f, 0.0f};
+#pragma unroll
+                for (int v = 0; v < kShrinkWaves; ++v) {
+                    const float2 u = *(reinterpret_cast<const float2 *>(&sums[b][v][of_c][of_lane]) + (t & 1));
+                    sum.x += u.x;
+                    sum.y += u.y;
+                }
+                sum.x = sum.x * alpha * col;
+                sum.y = sum.y * alpha * col;
+                if (b * 16 < ranks) *reinterpret_cast<float2 *>(to + b * 16) = sum;
+            }
         }
-    }
+        id = then;
+        turn = first;
+        if (id < 0) return false;
+        then = next(a.slots);
+        return true;
+    };
+    while (step(even, odd) && step(odd, even)) {}
 }
 
-constexpr int kExpandTileThreads = 256;
+// Waves of a workgroup: the more ranks, the more of them share what is made of t first.
+template <int RB> constexpr int kExpandTileWaves = RB < 4 ? 4 : 8;
 
-// A workgroup does 64 tokens and `rows` rows of Y, its waves 16 of them at a time.
+// A workgroup does 64 tokens and `rows` rows of Y (a multiple of 64), its waves 16 of them at a time; what such a block needs from memory is fetched while the one before it
+// is computed.
 // half: t is split into two halves, t = hi + lo, which the instruction's 32 steps take side by side for 16 ranks, beside the same 16 weights
 // twice: 22 bits of t, at a sixteenth of what binary32 instructions cost.  Every token's t is scaled by a power of two first, its largest
 // to 2^14 ... 2^15, so that neither half leaves its range: what lo loses below 2^-24 is 2^-39 of that largest.
-template <typename C, typename W, int RB> __global__ __launch_bounds__(kExpandTileThreads) void expand_tiles_kernel(const ExpandArgs a) {
+template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds__(kExpandTileWaves<RB> * 64, RB < 2 ? 3 : 2) void expand_tiles_kernel(const ExpandArgs a) {
     constexpr bool SCALED = std::is_same<C, int32_t>::value, HALF = std::is_same<W, _Float16>::value;
     typedef Step<W> Q;
     typedef typename Q::frag frag;
-    constexpr int PITCH = RB * 16 + 4;
+    constexpr int WAVES = kExpandTileWaves<RB>, PITCH = RB * 16 + 4, SHARE = WAVES * 64 / kTile;   // SHARE: threads of a token
     __shared__ __align__(16) float ts[kTile * PITCH];
-    __shared__ int exponents[kTile], list[kTile];
+    __shared__ __align__(16) frag operands[RB * 4][64];
+    __shared__ int exponents[kTile];
     const int tiles = (a.N + kTile - 1) / kTile, chunks = (a.M + a.rows - 1) / a.rows, task = task_of(blockIdx.x, tiles * chunks);
     if (task >= tiles * chunks) return;
     const int n0 = task % tiles * kTile, m0 = task / tiles * a.rows, end = min(a.M, m0 + a.rows);
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, i = lane & 15;
+    // Everything that waits for nothing is on its way first.
     const TileTokens tokens(a.index, a.count, n0, a.N, lane);
-    int count = 0;
-    {
-        int left[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) left[c] = tokens.id[c];
-        for (int id = TileTokens::next(left); id >= 0; id = TileTokens::next(left)) {
-            if (t == 0) list[count] = id;
-            ++count;
-        }
-    }
-    // ts[token]: by the tokens' order in the lanes, which a last tile's shifted columns change nothing about
-    gather_t<SCALED>(a, n0, min(kTile, a.N - n0), kExpandTileThreads, ts, PITCH);
-    __syncthreads();
-    if constexpr (HALF) {   // the tokens' exponents: four threads to a token
-        float top = 0.0f;
-        for (int j = t & 3; j < RB * 16; j += 4)
-            if (j < ranks16(a.rank) && n0 + (t >> 2) < a.N) top = larger(top, fabsf(ts[(t >> 2) * PITCH + j]));
-        top = larger(top, from_lane_xor<1>(top));
-        top = larger(top, from_lane_xor<2>(top));
-        if ((t & 3) == 0) exponents[t >> 2] = top > 0.0f && top < INFINITY ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
-        __syncthreads();
-    }
-    frag x[RB][4];
-    int down[4];   // the tokens' scaling, to be undone
-    const int ranks = ranks16(a.rank);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const int of = tokens.columns.first + c - n0;   // its row in ts: before the tile where a lane's first columns are not its own
-        const bool have = tokens.id[c] >= 0;
-        down[c] = HALF && have ? -exponents[of] : 0;
-#pragma unroll
-        for (int b = 0; b < RB; ++b)
-#pragma unroll
-            for (int e = 0; e < Q::LANE; ++e) {
-                const int j = b * 16 + (HALF ? (g & 1) * 8 : g * 4) + e;
-                const float v = have && j < ranks ? ts[of * PITCH + j] : 0.0f;
-                if constexpr (HALF) {
-                    const float scaled = __builtin_ldexpf(v, -down[c]);
-                    const _Float16 hi = (_Float16)scaled;
-                    const float rest = scaled - (float)hi;
-                    x[b][c][e] = g < 2 ? hi : rest - rest == 0.0f ? (_Float16)rest : (_Float16)0.0f;   // (an infinity has no rest)
-                } else {
-                    x[b][c][e] = v;
-                }
-            }
-    }
-    float col[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) col[c] = SCALED && a.col && tokens.columns.any ? a.col[(size_t)blockIdx.y * a.N + tokens.columns.first + c] : 1.0f;
+    GatherT<WAVES * 64, RB * 16> gather(a, n0, min(kTile, a.N - n0));
     const Matrix from(static_cast<const C *>(a.C) + (int64_t)blockIdx.y * a.M * a.ldc, a.M, a.N, a.ldc, sizeof(C));
     const Matrix Y(static_cast<W *>(a.Y) + (int64_t)blockIdx.y * a.M * a.ldy, a.M, a.N, a.ldy, sizeof(W));
     const Matrix rows(a.row, 1, a.M, a.M, 4);
-    const bool whole = a.rank % Q::LANE == 0;
-    for (int m = m0 + wave * 16; m < end; m += kExpandTileThreads / 64 * 16) {
-        C had[4][4];
-        float row[4];
+    // Offsets of a lane in a block; rows past M lie outside the matrices.  (What the lanes share, the block's first row, does not: a range is
+    // checked after it has been taken off.)
+    const bool any = tokens.columns.any;
+    uint32_t c_at[4], y_at[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int at = m + g * 4 + q;
-            load<C, 4>(from, at < end && tokens.columns.any ? ((uint32_t)at * (uint32_t)a.ldc + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(C) : kNowhere, 0, had[q]);
-            float one[1] = {1.0f};
-            if (SCALED && a.row) load<float, 1>(rows, at < end ? (uint32_t)at * 4u : kNowhere, 0, one);
-            row[q] = one[0];
-        }
-        float add[4][4];   // [row][token]
+    for (int q = 0; q < 4; ++q) {
+        c_at[q] = any ? ((uint32_t)(g * 4 + q) * (uint32_t)a.ldc + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(C) : kNowhere;
+        y_at[q] = any ? ((uint32_t)(g * 4 + q) * (uint32_t)a.ldy + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(W) : kNowhere;
+    }
+    struct Block { C had[4][4]; float row[4]; frag w[RB]; };
+    auto fetch_c = [&](int m, Block &b) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < 4; ++q) load<C, 4>(from, c_at[q], (uint32_t)m * (uint32_t)a.ldc * (uint32_t)sizeof(C), b.had[q]);
+        if constexpr (SCALED) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) add[q][c] = -0.0f;   // (what is added to nothing leaves it as it is)
-        for (int o = 0; o < count; ++o) {
-            const int id = __builtin_amdgcn_readfirstlane(list[o]);
-            const Matrix up(static_cast<const W *>(a.up) + (size_t)id * a.M * a.rank, a.M, a.rank, a.rank, sizeof(W));
-            frag w[RB];
-#pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const int j = b * 16 + (HALF ? (g & 1) * 8 : g * 4);
-                W v[Q::LANE];
-                weights<W, Q::LANE>(up, m + i < a.M && j < a.rank ? (uint32_t)(m + i) * (uint32_t)a.rank * (uint32_t)sizeof(W) : kNowhere, j, a.rank, whole, v);
-#pragma unroll
-                for (int e = 0; e < Q::LANE; ++e) w[b][e] = v[e];
+            for (int q = 0; q < 4; ++q) {
+                float one[1] = {1.0f};
+                if (a.row) load<float, 1>(rows, (uint32_t)(g * 4 + q) * 4u, (uint32_t)m * 4u, one);
+                b.row[q] = one[0];
             }
+        }
+    };
+    auto up_of = [&](int m, int id, frag (&w)[RB]) {
+        const Matrix up(static_cast<const W *>(a.up) + (size_t)id * a.M * a.rank, a.M, a.rank, a.rank, sizeof(W));
+        const uint32_t block_at = (uint32_t)m * (uint32_t)a.rank * (uint32_t)sizeof(W);
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            const int j = b * 16 + (HALF ? (g & 1) * 8 : g * 4);
+            const Piece<W> p = piece<W>(up, (uint32_t)i * (uint32_t)a.rank * (uint32_t)sizeof(W), block_at, j, a.rank, WHOLE);
+            __builtin_memcpy(&w[b], p.v, 16);
+        }
+    };
+    Block even, odd;
+    const int mine = m0 + wave * 16;
+    if (mine < end) fetch_c(mine, even);
+    int left[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) left[c] = tokens.id[c];
+    const int first = TileTokens::next(left), second = TileTokens::next(left);
+    bool all = true;   // have all tokens the first one?
+#pragma unroll
+    for (int c = 0; c < 4; ++c) all &= tokens.id[c] == first || !any || c < tokens.columns.skip;
+    all = __all(all);
+    auto fetch = [&](int m, Block &b) {
+        fetch_c(m, b);
+        if (first >= 0) up_of(m, first, b.w);
+    };
+    if (first >= 0 && mine < end) up_of(mine, first, even.w);
+    // Row (n % 4) * 16 + n / 4 of ts is token n of the tile: the lanes of a quarter read rows that follow each other.
+    auto row_of = [](int n) { return (n & 3) * 16 + (n >> 2); };
+    float top = gather.finish(ts, PITCH, row_of(gather.c));
+    if constexpr (HALF) {
+        top = larger(top, from_lane_xor<1>(top));
+        top = larger(top, from_lane_xor<2>(top));
+        if constexpr (SHARE == 8) top = larger(top, from_lane_xor<4>(top));
+        if (t % SHARE == 0) exponents[t / SHARE] = top > 0.0f && top < INFINITY ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
+    }
+    __syncthreads();
+    // The second operand of every instruction, one for each 16 ranks and each quarter of the tokens: a wave makes some of a quarter.
+    int down[4];   // the tokens' scaling, to be undone
+#pragma unroll
+    for (int c = 0; c < 4; ++c) down[c] = HALF && tokens.id[c] >= 0 ? -exponents[tokens.columns.first + c - n0] : 0;
+    {
+        const int q = wave & 3, id = q == 0 ? tokens.id[0] : q == 1 ? tokens.id[1] : q == 2 ? tokens.id[2] : tokens.id[3];
+        const int shift = q == 0 ? down[0] : q == 1 ? down[1] : q == 2 ? down[2] : down[3];
+        const int of = id >= 0 ? tokens.columns.first + q - n0 : 0;   // (a last lane's first columns may lie before the tile: they have no adapter)
+        const int ranks = ranks16(a.rank);
+#pragma unroll
+        for (int o = 0; o < RB * 4 / WAVES; ++o) {
+            const int b = o * (WAVES / 4) + (wave >> 2), j0 = b * 16 + (HALF ? (g & 1) * 8 : g * 4);
+            const float *const from = ts + row_of(of) * PITCH + j0;
+            float4v v[Q::LANE / 4];
+#pragma unroll
+            for (int p = 0; p < Q::LANE / 4; ++p) v[p] = id >= 0 && b * 16 < ranks ? *reinterpret_cast<const float4v *>(from + p * 4) : float4v{0.0f, 0.0f, 0.0f, 0.0f};
+            frag f;
+#pragma unroll
+            for (int e = 0; e < Q::LANE; ++e) {
+                if constexpr (HALF) {
+                    const float scaled = __builtin_ldexpf(v[e / 4][e % 4], -shift);
+                    const _Float16 hi = (_Float16)scaled;
+                    const float rest = scaled - (float)hi;
+                    f[e] = g < 2 ? hi : fabsf(rest) < INFINITY ? (_Float16)rest : (_Float16)0.0f;   // (an infinity has no rest)
+                } else {
+                    f[e] = v[e / 4][e % 4];
+                }
+            }
+            operands[b * 4 + q][lane] = f;
+        }
+    }
+    __syncthreads();
+    frag x[RB][4];
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[b][c] = operands[b * 4 + c][lane];
+    float col[4];
+    if constexpr (SCALED) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) col[c] = a.col && any ? a.col[(size_t)blockIdx.y * a.N + tokens.columns.first + c] : 1.0f;
+    }
+    auto block = [&](int m, const Block &b) {
+        float add[4][4];   // [row][token]
+        auto one = [&](int id, const frag (&w)[RB], bool every) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
+                const bool its = every || tokens.id[c] == id;
+                if (!every && !__any(its)) continue;
                 float4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int b = 0; b < RB; ++b) acc = Q::mma(w[b], x[b][c], acc);
-                if (tokens.id[c] == id)
+                for (int r = 0; r < RB; ++r) acc = Q::mma(w[r], x[r][c], acc);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) add[q][c] = HALF ? __builtin_ldexpf(acc[q], down[c]) : acc[q];
+                for (int q = 0; q < 4; ++q) {
+                    const float v = HALF ? __builtin_ldexpf(acc[q], down[c]) : acc[q];
+                    add[q][c] = its ? v : add[q][c];
+                }
+            }
+        };
+        if (all && first >= 0) {
+            one(first, b.w, true);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) add[q][c] = -0.0f;   // (what is added to nothing leaves it as it is)
+            // (The next adapter's weights are on their way while one is multiplied.)
+            frag w[RB];
+            if (second >= 0) up_of(m, second, w);
+            if (first >= 0) one(first, b.w, false);
+            int rest[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) rest[c] = left[c];
+            for (int id = second; id >= 0;) {
+                const int then = TileTokens::next(rest);
+                frag ahead[RB];
+                if (then >= 0) up_of(m, then, ahead);
+                one(id, w, false);
+                id = then;
+                if (id < 0) break;
+                const int last = TileTokens::next(rest);
+                if (last >= 0) up_of(m, last, w);
+                one(id, ahead, false);
+                id = last;
             }
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int at = m + g * 4 + q;
-            float c4[4];
             W y[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) c4[c] = (float)had[q][c];
-            finish<C, W, 4>(c4, col, row[q], add[q], y);
-            store<W, 4>(Y, at < end && tokens.columns.any ? ((uint32_t)at * (uint32_t)a.ldy + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(W) : kNowhere, 0,
-                        tokens.columns.any ? tokens.columns.skip : 0, y);
+            for (int c = 0; c < 4; ++c) {
+                float had = (float)b.had[q][c];
+                if constexpr (SCALED) had = had * col[c] * b.row[q];
+                y[c] = (W)(had + add[q][c]);
+            }
+            store<W, 4>(Y, y_at[q], (uint32_t)m * (uint32_t)a.ldy * (uint32_t)sizeof(W), any ? tokens.columns.skip : 0, y);
         }
+    };
+    constexpr int NEXT = WAVES * 16;
+    for (int m = mine; m < end; m += 2 * NEXT) {
+        if (m + NEXT < end) fetch(m + NEXT, odd);
+        block(m, even);
+        if (m + 2 * NEXT < end) fetch(m + 2 * NEXT, even);
+        if (m + NEXT < end) block(m + NEXT, odd);
     }
 }
 
@@ -471,42 +652,53 @@ namespace {
 
 struct Plan {   // the kernels of a call, and what they go by
     const void *shrink, *expand;
-    int parts, slots, tokens, rows;
+    int parts, turns, slots, rows;
     int64_t shrink_grid, expand_grid;
     int shrink_threads, expand_threads, expand_lds;
 };
 
+template <typename X, typename W, int RB> const void *shrink_tiles(bool whole) { return whole ? (const void *)shrink_tiles_kernel<X, W, RB, true> : (const void *)shrink_tiles_kernel<X, W, RB, false>; }
+template <typename C, typename W, int RB> const void *expand_tiles(bool whole) { return whole ? (const void *)expand_tiles_kernel<C, W, RB, true> : (const void *)expand_tiles_kernel<C, W, RB, false>; }
+template <typename C, typename W, int EACH> const void *expand_tokens(bool whole) { return whole ? (const void *)expand_tokens_kernel<C, W, EACH, true> : (const void *)expand_tokens_kernel<C, W, EACH, false>; }
+template <typename X, typename W, int V> const void *shrink_tokens(bool whole) { return whole ? (const void *)shrink_tokens_kernel<X, W, V, true> : (const void *)shrink_tokens_kernel<X, W, V, false>; }
+
 template <typename X, typename C, typename W> Plan plan_of(const sparsert_adapter_set &d) {
     Plan p{};
+    constexpr int LANE = 16 / (int)sizeof(W);
+    const bool whole_k = d.K % LANE == 0, whole_rank = d.rank % LANE == 0;
     const int ranks = (d.rank + 15) / 16 * 16;
-    static const int mode = getenv("AD_MODE") ? atoi(getenv("AD_MODE")) : 0;
-    static const int want = getenv("AD_WG") ? atoi(getenv("AD_WG")) : 128;
-    static const int ewant = getenv("AD_EWG") ? atoi(getenv("AD_EWG")) : 512;
-    if (d.N >= 4 && d.rank <= 64 && (mode == 2 || (mode == 0 && (int64_t)d.N * d.batch > 64))) {
+    // Bytes of weights that the tokens read if every one reads its own: what the first kind of kernels spends its time on.
+    const double own = (double)d.N * d.batch * ((double)d.M + d.K) * ranks * (int)sizeof(W);
+    const double limit = (30e6 + 4e6 * std::min(d.count, kTile)) * (sizeof(W) == 4 ? 2 : 1);
+    // (The tiles' lanes reckon with offsets of some rows on from any one.)
+    const bool near = (int64_t)(kShrinkWaves * Step<W>::ROWS) * d.ldx * (int)sizeof(X) < 1ll << 31 && 16ll * std::max((int64_t)d.ldc * (int)sizeof(C), (int64_t)d.ldy * (int)sizeof(W)) < 1ll << 31 &&
+                      64ll * d.K * (int)sizeof(W) < 1ll << 31 && 16ll * d.rank * (int)sizeof(W) < 1ll << 31;
+    if (near && d.N >= 4 && d.rank <= 64 && pieces_fit<W>(d.rank) && pieces_fit<W>(d.K) && own > limit) {
         const int64_t tiles = ((int64_t)d.N + kTile - 1) / kTile;
-        constexpr int unit = kShrinkWaves * Step<W>::ROWS;
-        int steps = 4;
-        auto parts = [&]() { return (d.K + unit * steps - 1) / (unit * steps); };
-        while (steps > 1 && tiles * d.batch * parts() < want) steps /= 2;
-        p.parts = parts();
-        p.slots = (int)std::min<int64_t>({8, d.count, std::max<int64_t>(1, 2 * want / (tiles * d.batch * p.parts))});
-        p.shrink = steps == 4 ? (const void *)shrink_tiles_kernel<X, W, 4> : steps == 2 ? (const void *)shrink_tiles_kernel<X, W, 2> : (const void *)shrink_tiles_kernel<X, W, 1>;
+        constexpr int TURN = kShrinkWaves * Step<W>::ROWS;
+        const int turns = (d.K + TURN - 1) / TURN;
+        p.parts = (int)std::min<int64_t>(turns, std::max<int64_t>(1, 64 / (tiles * d.batch)));
+        p.turns = (turns + p.parts - 1) / p.parts;
+        p.parts = (turns + p.turns - 1) / p.turns;
+        p.slots = (int)std::min<int64_t>({8, d.count, std::max<int64_t>(1, 256 / (tiles * d.batch * p.parts))});
+        p.shrink = ranks <= 16 ? shrink_tiles<X, W, 1>(whole_k) : ranks <= 32 ? shrink_tiles<X, W, 2>(whole_k) : shrink_tiles<X, W, 4>(whole_k);
         p.shrink_grid = tiles * p.parts * p.slots; p.shrink_threads = kShrinkWaves * 64;
-        p.expand = ranks <= 16 ? (const void *)expand_tiles_kernel<C, W, 1> : ranks <= 32 ? (const void *)expand_tiles_kernel<C, W, 2> : (const void *)expand_tiles_kernel<C, W, 4>;
-        p.tokens = kTile;
-        const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>((d.M + 63) / 64, ewant / (tiles * d.batch)));
-        p.rows = (int)(((d.M + chunks - 1) / chunks + 63) / 64 * 64);
-        p.expand_grid = tiles * ((d.M + p.rows - 1) / p.rows); p.expand_threads = kExpandTileThreads;
+        p.expand = ranks <= 16 ? expand_tiles<C, W, 1>(whole_rank) : ranks <= 32 ? expand_tiles<C, W, 2>(whole_rank) : expand_tiles<C, W, 4>(whole_rank);
+        const int step = ranks <= 32 ? kExpandTileWaves<2> * 16 : kExpandTileWaves<4> * 16;
+        const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>((d.M + step - 1) / step, (ranks <= 32 ? 512 : 256) / (tiles * d.batch)));
+        p.rows = (int)(((d.M + chunks - 1) / chunks + step - 1) / step * step);
+        p.expand_grid = tiles * ((d.M + p.rows - 1) / p.rows); p.expand_threads = step * 4;
         return p;
     }
     p.parts = (d.K + kTokenRows - 1) / kTokenRows;
-    p.tokens = std::min(kExpandTokens, 8192 / ranks);   // t of 32 KiB at most in LDS
-    p.rows = kExpandRows;
-    p.shrink = d.N < kTokenGroup ? (const void *)shrink_tokens_kernel<X, W, 1> : (const void *)shrink_tokens_kernel<X, W, kTokenGroup>;
-    p.expand = (const void *)expand_tokens_kernel<C, W>;
-    p.shrink_grid = ((int64_t)d.N + kTokenGroup - 1) / kTokenGroup * p.parts; p.shrink_threads = kTokenThreads;
-    p.expand_grid = ((int64_t)d.N + p.tokens - 1) / p.tokens * ((d.M + p.rows - 1) / p.rows); p.expand_threads = kExpandThreads;
-    p.expand_lds = (kExpandRows * (kExpandTokens + 1) + 16 + p.tokens * ranks) * (int)sizeof(float);
+    p.shrink = d.N < kTokenGroup ? shrink_tokens<X, W, 1>(d.K % 8 == 0) : shrink_tokens<X, W, kTokenGroup>(d.K % 8 == 0);
+    p.shrink_grid = ((int64_t)d.N + kTokenGroup - 1) / kTokenGroup * p.parts * (ranks / 16); p.shrink_threads = kTokenThreads;
+    const int64_t blocks = (d.M + kExpandRows - 1) / kExpandRows;
+    int each = 4;
+    while (each > 1 && (blocks * (((int64_t)d.N + each * kExpandWaves - 1) / (each * kExpandWaves)) * d.batch < 256 || each * kExpandWaves * ranks > 8192)) each /= 2;   // (t of 32 KiB at most in LDS)
+    p.expand = each == 4 ? expand_tokens<C, W, 4>(whole_rank) : each == 2 ? expand_tokens<C, W, 2>(whole_rank) : expand_tokens<C, W, 1>(whole_rank);
+    p.expand_grid = ((int64_t)d.N + each * kExpandWaves - 1) / (each * kExpandWaves) * blocks; p.expand_threads = kExpandThreads;
+    p.expand_lds = each * kExpandWaves * ranks * (int)sizeof(float);
     return p;
 }
 
@@ -525,10 +717,10 @@ int launch_adapters(const AdaptersCall &c, std::string &err) {
     const Plan p = plan_of(d);
     if (p.shrink_grid >= 1ll << 30 || p.expand_grid >= 1ll << 30) { err = "too many workgroups"; return SPARSERT_EUNSUPPORTED; }
     float *const t = static_cast<float *>(c.workspace);
-    ShrinkArgs s{c.X, c.down, c.index, t, d.K, d.N, d.ldx, d.rank, d.count, p.parts, p.slots};
+    ShrinkArgs s{c.X, c.down, c.index, c.alpha, c.col, t, d.K, d.N, d.ldx, d.rank, d.count, p.parts, p.turns, p.slots};
     const auto grid = [&](int64_t n) { return dim3((uint32_t)((n + 7) / 8 * 8), (uint32_t)d.batch); };
     if (int rc = launch_operator(p.shrink, grid(p.shrink_grid), p.shrink_threads, s, c.stream, err)) return rc;
-    ExpandArgs e{c.C, c.up, c.index, c.alpha, c.row, c.col, t, c.Y, d.M, d.N, d.ldc, d.ldy, d.count, p.parts, p.rows, (int16_t)p.tokens, (int16_t)d.rank};
+    ExpandArgs e{c.C, c.up, c.index, c.row, c.col, t, c.Y, d.M, d.N, d.ldc, d.ldy, d.count, p.parts, p.rows, d.rank};
     return launch_operator(p.expand, grid(p.expand_grid), p.expand_threads, e, c.stream, err, p.expand_lds);
 }
 
