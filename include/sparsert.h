@@ -410,7 +410,7 @@ void sparsert_plan_destroy(sparsert_plan *plan);
  * borrowed and must not overlap what a call writes, except where an operator names a buffer that may be the same.  Columns behind
  * the N of a wider pitch are neither read nor written.
  * Errors: EINVAL (null or misaligned pointer, sizes that are not positive, a pitch under N, a type the operator does not
- * take, reserved fields set), EUNSUPPORTED (one matrix of a problem of 2 GiB and more), EHIP.
+ * take, reserved fields set), EUNSUPPORTED (one matrix of a problem of 2 GiB and more; 2^28 rows or tokens and more), EHIP.
  */
 
 /* Root-mean-square norm over the rows (features) of every column (token). */
@@ -494,7 +494,8 @@ typedef struct sparsert_adapter_set {
  *
  * where x = X and c = C or, for int8 X, x[k,n] = X[k,n] * col_scale[n] and c[m,n] = C[m,n] * col_scale[n] * row_scale[m]:
  * the call is then given what sparsert_spmm was given and what it wrote, and takes sparsert_dequantize's place.
- * Sums are binary32, t is kept in binary32, Y is rounded once.  A token is computed from its own column and adapter alone:
+ * Sums are binary32 and Y is rounded once.  alpha[a] * t is kept in binary32, or, for many tokens of half weights, in two halves (22 bits
+ * of it, and whatever is over 2^-39 of the token's largest).  A token is computed from its own column and adapter alone:
  * what is infinite or undefined elsewhere does not reach it.
  *
  *   X_dev          [batch, K, ldx]

@@ -11,7 +11,7 @@ namespace {
 using sparsert::set_error;
 
 constexpr int64_t kProblemBytes = 1ll << 31;   // kernels address one problem's matrix with 32-bit byte offsets
-constexpr int32_t kMaxRank = 256;
+constexpr int32_t kMaxRank = 256, kMost = 1 << 28;   // (a vector of floats as long stays under that, too)
 
 int size_of(int32_t dtype) { return dtype == SPARSERT_F32 ? 4 : dtype == SPARSERT_F16 ? 2 : 1; }
 bool floating(int32_t dtype) { return dtype == SPARSERT_F32 || dtype == SPARSERT_F16; }
@@ -20,6 +20,7 @@ template <typename... P> bool misaligned(uintptr_t mask, P... p) { return ((... 
 
 int check_sizes(int32_t rows, int32_t N, int32_t &batch, const int32_t *reserved, int n) {
     if (rows < 1 || N < 1) return set_error(SPARSERT_EINVAL, "sizes must be positive");
+    if (rows >= kMost || N >= kMost) return set_error(SPARSERT_EUNSUPPORTED, "2^28 rows or tokens, or more");
     if (batch < 0 || batch > 65535) return set_error(SPARSERT_EINVAL, "batch must be 0..65535");
     if (batch == 0) batch = 1;
     for (int i = 0; i < n; ++i)
@@ -50,7 +51,7 @@ int check_norm(sparsert_norm &d) {
 
 int check_set(sparsert_adapter_set &d) {
     if (int rc = check_sizes(d.M, d.N, d.batch, d.reserved, 3)) return rc;
-    if (d.K < 1) return set_error(SPARSERT_EINVAL, "sizes must be positive");
+    if (int rc = check_sizes(d.K, d.N, d.batch, d.reserved, 0)) return rc;
     if (!floating(d.dtype)) return set_error(SPARSERT_EINVAL, "dtype must be F32 or F16");
     if (d.x_dtype != d.dtype && d.x_dtype != SPARSERT_I8) return set_error(SPARSERT_EINVAL, "x_dtype must be dtype or I8");
     if (d.rank < 1 || d.rank > kMaxRank) return set_error(SPARSERT_EINVAL, "rank must be 1..256");

@@ -74,7 +74,7 @@ def adapters(x, down, up, index, alpha, c, row, col):
 
 def check_adapters(y, x, down, up, index, alpha, c, row, col):
     want, size = adapters(x, down, up, index, alpha, c, row, col)
-    # K and rank terms to a sum, factors and additions; t may be held to 22 bits (4 u)
+    # K and rank terms to a sum, factors and additions; t may be held to 22 bits (4 u), which the 16 cover
     bound = size * (x.shape[-2] + down.shape[1] + 16) * U + store_bound(want, y.dtype)
     off = np.abs(y.astype(np.float64) - want)
     assert (off <= bound * 1.001).all(), (np.max(off / np.maximum(bound, 1e-300)), np.argwhere(off > bound)[:4])

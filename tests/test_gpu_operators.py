@@ -285,6 +285,75 @@ def test_adapters_of_real_sizes(M, K, N, rank, count, index, kind):
     assert call.read().tobytes() == y.tobytes()     # the same operands, the same bits
 
 
+# Calls whose tokens would read more weights than their tiles of 64 share go to the matrix cores: over 34 MB with one adapter, 4 MB more for each other one, twice that in single precision.
+@pytest.mark.parametrize("kind", ["f16", "f32", "i8f16", "i8f32"])
+@pytest.mark.parametrize("M,K,N,rank,count,batch,index", [
+    (520, 512, 1100, 64, 3, 1, "runs"), (517, 513, 1101, 64, 2, 1, "runs"), (500, 600, 1500, 64, 40, 1, "tokens"), (530, 600, 1063, 33, 3, 1, "tokens"),
+    (300, 270, 2050, 4, 1, 2, "runs"), (301, 263, 4103, 6, 2, 1, "runs"), (1030, 264, 1200, 24, 2, 1, "tokens"), (700, 1300, 450, 20, 1, 3, "runs"),
+    (17, 9, 10303, 64, 1, 1, "runs"), (3, 1025, 1130, 40, 1, 1, "tokens"), (2100, 8, 700, 62, 1, 1, "runs"), (64, 4100, 257, 57, 2, 1, "runs"), (1000, 1000, 64, 64, 1, 5, "runs"),
+    (900, 900, 65, 64, 1, 5, "tokens")])
+def test_adapters_of_many_tokens(M, K, N, rank, count, batch, index, kind):
+    call = AdaptersCall(adapters_case(np.random.default_rng(M + N), M, K, N, rank, count, kind, batch, index), pads=(0, 0, 0) if N % 2 == 0 else (1, 2, 3))
+    call.run()
+    y = call.read()
+    call.check(y)
+    call.run()
+    assert call.read().tobytes() == y.tobytes()
+
+
+@pytest.mark.parametrize("kind", ["f16", "f32"])
+def test_many_tokens_are_computed_from_their_own_column_and_adapter_alone(kind):
+    rng = np.random.default_rng(18)
+    N = 1100
+    s = adapters_case(rng, 520, 514, N, 63, 4, kind)
+    s["index"][0, :] = np.where(np.arange(N) < 300, np.arange(N) // 150, np.arange(N) % 7 - 2)     # runs, then requests of a token each, some without adapter
+    s["index"][0, 700:800] = -1
+    s["index"][0, 800:900] = np.where(np.arange(100) % 2, 4, np.iinfo(np.int32).min)
+    clean = {k: None if v is None else v.copy() for k, v in s.items()}
+    hurt = [0, 150, 331, 1099]
+    s["index"][0, 331], clean["index"][0, 331] = 1, 1
+    s["x"][0, 513, 0], s["x"][0, 5, 150], s["x"][0, 0, 331], s["x"][0, 77, 1099] = np.nan, np.inf, -np.inf, np.nan
+    s["index"][0, 1099], clean["index"][0, 1099] = 0, 0
+    s["down"][3, 62, 513], s["up"][3, 519, 62] = np.inf, np.nan                # the last weights of adapter 3, which is the last
+    s["down"][2, 0, 0] = np.nan
+    got, want = (AdaptersCall(v, pads=(1, 1, 1)) for v in (s, clean))
+    got.run()
+    want.run()
+    want.check(want.read())
+    sound = ~np.isin(s["index"][0], (2, 3))
+    sound[hurt] = False
+    a, b = got.read(), want.read()
+    assert np.array_equal(a[..., sound], b[..., sound])
+    assert not np.isfinite(a[0][:, hurt]).any()
+    none = (s["index"][0] < 0) | (s["index"][0] >= 4)
+    assert none.sum() > 200 and np.array_equal(a[..., none], s["c"][..., none])
+
+
+@pytest.mark.parametrize("kind", ["f16", "f32", "i8f32"])
+def test_adapters_of_many_tokens_in_place(kind):
+    rng = np.random.default_rng(19)
+    s = adapters_case(rng, 530, 512, 1101, 64, 2, kind, index="runs")
+    s["alpha"] = None
+    call = AdaptersCall(s, pads=(3, 2, 2), inplace=True)
+    call.run()
+    call.check(call.read())
+
+
+def test_many_tokens_keep_large_and_small_inner_values():
+    rng = np.random.default_rng(20)
+    s = adapters_case(rng, 520, 512, 1100, 64, 1, "f16")
+    s["index"][:] = 0
+    s["x"] *= np.float16(1500.0)
+    s["down"] = (s["down"].astype(np.float32) * 60).astype(np.float16)
+    s["up"] = (s["up"].astype(np.float32) * 1e-3).astype(np.float16)
+    s["x"][0, :, ::3] = (s["x"][0, :, ::3].astype(np.float32) * 1e-9).astype(np.float16)      # tokens of very different sizes side by side
+    s["x"][0, :, 7] = 0
+    assert np.abs(s["down"][0].astype(np.float64) @ s["x"][0].astype(np.float64)).max() > 70000
+    call = AdaptersCall(s)
+    call.run()
+    call.check(call.read())
+
+
 @pytest.mark.parametrize("kind", ["f16", "f32", "i8f16"])
 def test_adapters_where_no_token_has_one_and_where_the_index_names_none(kind):
     rng = np.random.default_rng(2)

@@ -47,7 +47,8 @@ def norm(**kw):
     (dict(dtype=sp.I8), sp.EINVAL, "dtype"), (dict(dtype=7), sp.EINVAL, "dtype"), (dict(out_dtype=sp.F32), sp.EINVAL, "out_dtype"),
     (dict(eps=0.0), sp.EINVAL, "eps"), (dict(eps=-1.0), sp.EINVAL, "eps"), (dict(eps=float("nan")), sp.EINVAL, "eps"), (dict(eps=float("inf")), sp.EINVAL, "eps"),
     (dict(ldx=15), sp.EINVAL, "ldx"), (dict(ldh=-1), sp.EINVAL, "ldh"), (dict(ldy=1), sp.EINVAL, "ldy"),
-    (dict(K=1 << 20, ldx=1 << 10), sp.EUNSUPPORTED, "2 GiB"), (dict(K=2 ** 31 - 1, N=2 ** 31 - 1), sp.EUNSUPPORTED, "2 GiB")])
+    (dict(K=1 << 20, ldx=1 << 10), sp.EUNSUPPORTED, "2 GiB"), (dict(K=2 ** 31 - 1, N=2 ** 31 - 1), sp.EUNSUPPORTED, "2^28"),
+    (dict(K=1 << 28, N=1), sp.EUNSUPPORTED, "2^28"), (dict(K=1, N=1 << 28), sp.EUNSUPPORTED, "2^28")])
 def test_norm_descriptors_that_are_refused(kw, status, text):
     refused(status, text, sp.rms_norm, norm(**kw), P, 0, 0, 0, Q)
     refused(status, text, norm(**kw).workspace_bytes)
@@ -82,7 +83,8 @@ def test_norm_calls_that_are_refused():
 
 @pytest.mark.parametrize("kw,status,text", [
     (dict(M=0), sp.EINVAL, "positive"), (dict(N=0), sp.EINVAL, "positive"), (dict(batch=70000), sp.EINVAL, "batch"), (dict(dtype=sp.I8), sp.EINVAL, "dtype"),
-    (dict(ldc=15), sp.EINVAL, "ldc"), (dict(ldy=15), sp.EINVAL, "ldy"), (dict(M=1 << 20, ldc=512), sp.EUNSUPPORTED, "2 GiB")])
+    (dict(ldc=15), sp.EINVAL, "ldc"), (dict(ldy=15), sp.EINVAL, "ldy"), (dict(M=1 << 20, ldc=512), sp.EUNSUPPORTED, "2 GiB"),
+    (dict(M=1, N=1 << 28), sp.EUNSUPPORTED, "2^28")])
 def test_dequantize_descriptors_that_are_refused(kw, status, text):
     a = dict(M=8, N=16)
     a.update(kw)
@@ -112,7 +114,8 @@ def adapter_set(**kw):
     (dict(rank=0), sp.EINVAL, "rank"), (dict(rank=257), sp.EINVAL, "rank"), (dict(count=0), sp.EINVAL, "count"), (dict(dtype=sp.I8), sp.EINVAL, "dtype"),
     (dict(x_dtype=sp.F32), sp.EINVAL, "x_dtype"), (dict(ldx=15), sp.EINVAL, "ldx"), (dict(ldc=15), sp.EINVAL, "ldc"), (dict(ldy=15), sp.EINVAL, "ldy"),
     (dict(M=1 << 20, N=1024), sp.EUNSUPPORTED, "2 GiB"), (dict(K=1 << 24, rank=256, N=1), sp.EUNSUPPORTED, "2 GiB"),
-    (dict(M=1, K=1, N=1 << 26, batch=64), sp.EUNSUPPORTED, "tokens")])
+    (dict(M=1, K=1, N=1 << 26, batch=64), sp.EUNSUPPORTED, "tokens"), (dict(M=1 << 28, K=1, N=1), sp.EUNSUPPORTED, "2^28"),
+    (dict(M=1, K=1 << 28, N=1), sp.EUNSUPPORTED, "2^28"), (dict(M=1, K=1, N=1 << 28, x_dtype=sp.I8), sp.EUNSUPPORTED, "2^28")])
 def test_adapter_sets_that_are_refused(kw, status, text):
     refused(status, text, adapter_set(**kw).workspace_bytes)
     refused(status, text, sp.adapters, adapter_set(**kw), P, P, P, P, 0, Q, 0, 0, S, T, 1 << 40)
