@@ -715,10 +715,12 @@ size_t adapters_workspace(const sparsert_adapter_set &d) { return (size_t)d.batc
 int launch_adapters(const AdaptersCall &c, std::string &err) {
     const sparsert_adapter_set &d = c.d;
     const Plan p = plan_of(d);
-    if (p.shrink_grid >= 1ll << 30 || p.expand_grid >= 1ll << 30) { err = "too many workgroups"; return SPARSERT_EUNSUPPORTED; }
+    const auto whole = [](int64_t n) { return (n + 7) / 8 * 8; };
+    if (int rc = check_launch(whole(p.shrink_grid), p.shrink_threads, err)) return rc;
+    if (int rc = check_launch(whole(p.expand_grid), p.expand_threads, err)) return rc;
     float *const t = static_cast<float *>(c.workspace);
     ShrinkArgs s{c.X, c.down, c.index, c.alpha, c.col, t, d.K, d.N, d.ldx, d.rank, d.count, p.parts, p.turns, p.slots};
-    const auto grid = [&](int64_t n) { return dim3((uint32_t)((n + 7) / 8 * 8), (uint32_t)d.batch); };
+    const auto grid = [&](int64_t n) { return dim3((uint32_t)whole(n), (uint32_t)d.batch); };
     if (int rc = launch_operator(p.shrink, grid(p.shrink_grid), p.shrink_threads, s, c.stream, err)) return rc;
     ExpandArgs e{c.C, c.up, c.index, c.row, c.col, t, c.Y, d.M, d.N, d.ldc, d.ldy, d.count, p.parts, p.rows, d.rank};
     return launch_operator(p.expand, grid(p.expand_grid), p.expand_threads, e, c.stream, err, p.expand_lds);

@@ -80,7 +80,6 @@ int launch_dequantize(const DequantCall &c, std::string &err) {
     const int vectors = (int)(((int64_t)d.N + V - 1) / V), lanes = vectors > 16 ? 64 : vectors > 4 ? 16 : vectors > 1 ? 4 : 1;
     const int64_t strips = (vectors + lanes - 1) / lanes, rows = kDequantThreads / lanes;
     const int64_t blocks = (d.M + rows * a.passes - 1) / (rows * a.passes), tasks = strips * blocks;
-    if (tasks >= 1ll << 30) { err = "too many workgroups"; return SPARSERT_EUNSUPPORTED; }
     const bool half = d.dtype == SPARSERT_F16;
     const void *kernel = V == 1 ? half ? dequantize_of<_Float16, 1>(lanes) : dequantize_of<float, 1>(lanes) : half ? dequantize_of<_Float16, 4>(lanes) : dequantize_of<float, 4>(lanes);
     return launch_operator(kernel, dim3((uint32_t)((tasks + 7) / 8 * 8), (uint32_t)d.batch), kDequantThreads, a, c.stream, err);

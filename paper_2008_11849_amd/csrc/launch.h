@@ -8,6 +8,13 @@
 
 namespace sparsert {
 
+// A launch has under 2^32 threads along x.
+inline int check_launch(int64_t workgroups, int threads, std::string &err) {
+    if (workgroups * threads < 1ll << 32) return SPARSERT_OK;
+    err = "more workgroups than a launch can have";
+    return SPARSERT_EUNSUPPORTED;
+}
+
 template <typename Args>
 int launch_operator(const void *kernel, dim3 grid, int threads, Args &args, void *stream, std::string &err, int lds_bytes = 0) {
     static_assert(sizeof(Args) <= kArgBytes, "a longer argument block costs the host more per launch");

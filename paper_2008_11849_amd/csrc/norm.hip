@@ -373,8 +373,9 @@ int launch_norm(const NormCall &c, std::string &err) {
     const bool half = d.dtype == SPARSERT_F16, quant = d.out_dtype == SPARSERT_I8;
     const void *kernel = half ? quant ? norm_of<_Float16, true>(d, columns) : norm_of<_Float16, false>(d, columns)
                               : quant ? norm_of<float, true>(d, columns) : norm_of<float, false>(d, columns);
-    const int strips = (int)(((int64_t)d.N + columns - 1) / columns);
-    return launch_operator(kernel, dim3((uint32_t)((strips + 7) / 8 * 8), (uint32_t)d.batch), kNormThreads, a, c.stream, err);
+    const int64_t strips = ((int64_t)d.N + columns - 1) / columns, workgroups = (strips + 7) / 8 * 8;
+    if (int rc = check_launch(workgroups, kNormThreads, err)) return rc;
+    return launch_operator(kernel, dim3((uint32_t)workgroups, (uint32_t)d.batch), kNormThreads, a, c.stream, err);
 }
 
 bool stream_of_current_device(void *stream) {

@@ -146,6 +146,12 @@ def test_adapters_calls_that_are_refused():
     assert sp.raw.sparsert_adapters_workspace(adapter_set().handle, None) == sp.EINVAL
 
 
+def test_more_workgroups_than_a_launch_can_have_are_refused():
+    refused(sp.EUNSUPPORTED, "workgroups", sp.rms_norm, sp.RmsNorm(1, (1 << 28) - 1, dtype=sp.F32), P, 0, 0, 0, Q, 0, 0, 0)
+    refused(sp.EUNSUPPORTED, "workgroups", sp.adapters, adapter_set(M=1, K=1, N=(1 << 28) - 1), P, P, P, P, 0, Q, 0, 0, S, T, 1 << 40)
+    refused(sp.EUNSUPPORTED, "workgroups", sp.adapters, adapter_set(M=1, K=200, N=1 << 22, rank=256), P, P, P, P, 0, Q, 0, 0, S, T, 1 << 40)
+
+
 @pytest.mark.parametrize("source", ["norm.hip", "dequantize.hip", "adapters.hip"])
 def test_wide_stores_have_no_scalar_offset(source, tmp_path):
     """Behind a buffer store of 12 or 16 bytes with a scalar offset the compiler leaves no room before the data registers are written anew."""
