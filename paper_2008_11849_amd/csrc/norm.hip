@@ -84,7 +84,7 @@ template <typename T, int V, int L, int THREADS> struct Rows {
 #pragma unroll
             for (int v = 0; v < V; ++v) h[i][v] = (float)x[i][v] + (float)r[i][v];
     }
-    template <typename Out, int PASSES, typename F> __device__ __forceinline__ void write(const Matrix &m, int k0, int ld, F value) const {
+    template <typename Out, int PASSES, int AUX = 0, typename F> __device__ __forceinline__ void write(const Matrix &m, int k0, int ld, F value) const {
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
             Out out[V];
@@ -92,7 +92,7 @@ template <typename T, int V, int L, int THREADS> struct Rows {
             for (int v = 0; v < V; ++v) out[v] = value(i, v);
             uint32_t common;
             const uint32_t at = place(k0, i, ld, sizeof(Out), common);
-            store<Out, V>(m, at, common, columns.any ? columns.skip : 0, out);
+            store<Out, V, AUX>(m, at, common, columns.any ? columns.skip : 0, out);
         }
     }
 };
@@ -223,7 +223,7 @@ template <typename T, bool QUANT, int V, int L> __global__ __launch_bounds__(kPa
     }
 }
 
-template <typename T, bool QUANT, int V, int L> __global__ __launch_bounds__(kPartThreads) void norm_results_kernel(const NormArgs a) {
+template <typename T, bool QUANT, int V, int L, bool FAR> __global__ __launch_bounds__(kPartThreads) void norm_results_kernel(const NormArgs a) {
     typedef out_t<T, QUANT> Out;
     typedef Rows<T, V, L, kPartThreads> Part;
     constexpr int W = V * L, GROUPS = kPartThreads / W;
@@ -274,7 +274,7 @@ template <typename T, bool QUANT, int V, int L> __global__ __launch_bounds__(kPa
     for (int k0 = p.first; k0 < p.end; k0 += kPartPasses * Part::ROWS) {
         float h[kPartPasses][V], g[kPartPasses];
         p.fetch(k0, h, g);
-        if (a.H) p.template write<T, kPartPasses>(H, k0, a.ldh, [&](int i, int v) { return (T)h[i][v]; });
+        if (a.H) p.template write<T, kPartPasses, FAR ? 2 : 0>(H, k0, a.ldh, [&](int i, int v) { return (T)h[i][v]; });
         p.template write<Out, kPartPasses>(Y, k0, a.ldy, [&](int i, int v) { return result<Out>(h[i][v] * g[i], f[v]); });
     }
 }
@@ -326,14 +326,14 @@ template <typename T> double one_kernel_us(const sparsert_norm &d, double bytes)
 
 struct SplitNorm { int parts, rows, strips; const void *sums, *results; };
 
-template <typename T, bool QUANT, int V, int L> SplitNorm split_with(const sparsert_norm &d, int workgroups) {
+template <typename T, bool QUANT, int V, int L, bool FAR = false> SplitNorm split_with(const sparsert_norm &d, int workgroups) {
     constexpr int W = V * L, ROWS = kPartThreads / L;
     const int strips = (int)(((int64_t)d.N + W - 1) / W);
     // No more parts than a workgroup fetches the sums of at once.
     const int64_t most = std::min<int64_t>((d.K + ROWS - 1) / ROWS, kPartThreads / W * kPartsAtOnce);
     const int64_t parts = std::min(most, std::max<int64_t>(1, workgroups / ((int64_t)strips * d.batch)));
     const int rows = (int)((d.K + parts - 1) / parts);
-    return {(d.K + rows - 1) / rows, rows, strips, (const void *)norm_sums_kernel<T, QUANT, V, L>, (const void *)norm_results_kernel<T, QUANT, V, L>};
+    return {(d.K + rows - 1) / rows, rows, strips, (const void *)norm_sums_kernel<T, QUANT, V, L>, (const void *)norm_results_kernel<T, QUANT, V, L, FAR>};
 }
 
 template <typename T, bool QUANT> SplitNorm split_of(const sparsert_norm &d) {
@@ -342,7 +342,7 @@ template <typename T, bool QUANT> SplitNorm split_of(const sparsert_norm &d) {
     if (one_kernel_us<T>(d, bytes) <= (QUANT ? 6.2 : 5.3) + bytes / 4.4e6) return {};
     if (d.N < V) return d.N > 4 ? split_with<T, QUANT, 1, 8>(d, 256) : d.N > 2 ? split_with<T, QUANT, 1, 4>(d, 256) : split_with<T, QUANT, 1, 2>(d, 256);
     constexpr int64_t wide = V * kWideLanes;
-    if (bytes > 40e6 && d.batch * (d.N / wide) * (kPartThreads / wide * kPartsAtOnce) >= 256) return split_with<T, QUANT, V, kWideLanes>(d, 512);
+    if (bytes > 40e6 && d.batch * (d.N / wide) * (kPartThreads / wide * kPartsAtOnce) >= 256) return bytes > 100e6 ? split_with<T, QUANT, V, kWideLanes, true>(d, 512) : split_with<T, QUANT, V, kWideLanes>(d, 512);
     return d.N > 4 * V ? split_with<T, QUANT, V, 8>(d, 256) : d.N > 2 * V ? split_with<T, QUANT, V, 4>(d, 256)
          : d.N > V ? split_with<T, QUANT, V, 2>(d, 256) : split_with<T, QUANT, V, 1>(d, 256);
 }

@@ -47,22 +47,23 @@ template <typename T, int V> __device__ __forceinline__ void load(const Matrix &
 // The same for results; the first `skip` of them belong to another lane.
 // The offset of a store is one register: behind a store of 16 bytes with a scalar offset the compiler lets the next instruction overwrite
 // the data at once, and of the first four bytes the last lanes of every sixteen then stored the new ones.  With none it keeps a clock between.
-template <typename T, int V> __device__ __forceinline__ void store(const Matrix &m, uint32_t lane, uint32_t common, int skip, const T (&from)[V]) {
+// AUX: cache policy (2: not to be kept).
+template <typename T, int V, int AUX = 0> __device__ __forceinline__ void store(const Matrix &m, uint32_t lane, uint32_t common, int skip, const T (&from)[V]) {
     typedef typename Raw<(int)sizeof(T) * V>::type raw;
     const uint32_t at = lane + common;   // (kNowhere plus a part under 2 GiB stays out of every range)
     if (skip == 0) {
         raw r;
         __builtin_memcpy(&r, from, sizeof(raw));
-        if constexpr (sizeof(raw) == 16) __builtin_amdgcn_raw_buffer_store_b128(r, m.at, at, 0, 0);
-        else if constexpr (sizeof(raw) == 8) __builtin_amdgcn_raw_buffer_store_b64(r, m.at, at, 0, 0);
-        else if constexpr (sizeof(raw) == 4) __builtin_amdgcn_raw_buffer_store_b32(r, m.at, at, 0, 0);
-        else if constexpr (sizeof(raw) == 2) __builtin_amdgcn_raw_buffer_store_b16(r, m.at, at, 0, 0);
-        else __builtin_amdgcn_raw_buffer_store_b8(r, m.at, at, 0, 0);
+        if constexpr (sizeof(raw) == 16) __builtin_amdgcn_raw_buffer_store_b128(r, m.at, at, 0, AUX);
+        else if constexpr (sizeof(raw) == 8) __builtin_amdgcn_raw_buffer_store_b64(r, m.at, at, 0, AUX);
+        else if constexpr (sizeof(raw) == 4) __builtin_amdgcn_raw_buffer_store_b32(r, m.at, at, 0, AUX);
+        else if constexpr (sizeof(raw) == 2) __builtin_amdgcn_raw_buffer_store_b16(r, m.at, at, 0, AUX);
+        else __builtin_amdgcn_raw_buffer_store_b8(r, m.at, at, 0, AUX);
     } else if constexpr (V > 1) {
 #pragma unroll
         for (int v = 1; v < V; ++v) {
             const T one[1] = {from[v]};
-            store<T, 1>(m, v >= skip ? lane + (uint32_t)v * (uint32_t)sizeof(T) : kNowhere, common, 0, one);
+            store<T, 1, AUX>(m, v >= skip ? lane + (uint32_t)v * (uint32_t)sizeof(T) : kNowhere, common, 0, one);
         }
     }
 }
