@@ -507,8 +507,9 @@ typedef struct sparsert_adapter_set {
  *   row_scale_dev  float[M], col_scale_dev float[batch, N]: int8 X only (NULL = ones), NULL otherwise
  *   Y_dev          [batch, M, ldy]; may be C_dev where both have elements of one size and ldy == ldc
  *   workspace_dev  DEVICE, 16-byte aligned, at least the bytes that sparsert_adapters_workspace reports (EINVAL if
- *                  workspace_bytes is less).  Holds t between the call's two kernels, nothing from call to call: calls that
- *                  may run at the same time (two streams, two graphs) need one each
+ *                  workspace_bytes is less), or NULL where that is 0: a single token of a small adapter is one kernel.  Holds t
+ *                  between the call's two kernels, nothing from call to call: calls that may run at the same time (two streams,
+ *                  two graphs) need one each
  */
 int sparsert_adapters_workspace(const sparsert_adapter_set *set, size_t *bytes);
 int sparsert_adapters(const sparsert_adapter_set *set, const void *X_dev, const void *down_dev, const void *up_dev,

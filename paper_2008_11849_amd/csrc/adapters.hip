@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.h"
 #include "operators.h"
@@ -65,25 +66,45 @@ template <typename W> __device__ __forceinline__ Piece<W> piece(const Matrix &m,
 // Can rows of `end` elements be read so?
 template <typename W> bool pieces_fit(int end) { return end >= 16 / (int)sizeof(W) || end * sizeof(W) % 4 == 0; }
 
-// The same for V elements and rows of any length.
-template <typename W, int V> __device__ __forceinline__ void weights(const Matrix &m, uint32_t row_at, int at, int end, bool whole, W (&to)[V]) {
-    constexpr int LANE = 16 / sizeof(W);
-    if (whole || end >= LANE) {
+// The same for the kernels that multiply a lane's piece of many rows with numbers of its own: a piece that the end cuts short is the row's last 16 bytes as they
+// lie, without what belongs to the lane before, and the lane moves its numbers instead (2.6 us less than moving the weights, for 16 rows of half weights).
+template <typename W, bool WHOLE> struct Cut {
+    static constexpr int LANE = 16 / sizeof(W), EACH = 4 / sizeof(W);
+    int from, end;
+    bool any;
+    uint32_t keep[4];
+    __device__ __forceinline__ Cut(int at, int end) : from(WHOLE ? at : max(min(at, end - LANE), 0)), end(end), any(at < end) {
+        if constexpr (!WHOLE)
 #pragma unroll
-        for (int p = 0; p < V / LANE; ++p) {
-            const Piece<W> q = piece<W>(m, row_at, 0, at + p * LANE, end, whole);
+            for (int d = 0; d < 4; ++d) {
+                keep[d] = 0;
 #pragma unroll
-            for (int i = 0; i < LANE; ++i) to[p * LANE + i] = q.v[i];
+                for (int h = 0; h < EACH; ++h)
+                    if (from + d * EACH + h >= at && from + d * EACH + h < end) keep[d] |= EACH == 1 ? ~0u : 0xffffu << (h * 16);
+            }
+    }
+    __device__ __forceinline__ bool keeps(int i) const { return WHOLE ? any : (keep[i / EACH] >> (i % EACH * 16) & 1) != 0; }
+    __device__ __forceinline__ void load(const Matrix &m, uint32_t row_at, W (&to)[LANE]) const {
+        const uint32_t at = any ? row_at + (uint32_t)from * (uint32_t)sizeof(W) : kNowhere;
+        if (WHOLE || end >= LANE) {
+            sparsert::load<W, LANE>(m, at, 0, to);
+        } else {   // (ranges are checked in steps of four bytes, so that 16 bytes may leave out the last half of a matrix)
+#pragma unroll
+            for (int i = 0; i < LANE; ++i) {
+                W one[1];
+                sparsert::load<W, 1>(m, any && i < end ? at + (uint32_t)i * (uint32_t)sizeof(W) : kNowhere, 0, one);
+                to[i] = one[0];
+            }
         }
-    } else {
+        if constexpr (!WHOLE) {
+            uint32_t u[4];
+            __builtin_memcpy(u, to, 16);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            W one[1];
-            load<W, 1>(m, at + i < end ? row_at + (uint32_t)(at + i) * (uint32_t)sizeof(W) : kNowhere, 0, one);
-            to[i] = one[0];
+            for (int d = 0; d < 4; ++d) u[d] &= keep[d];
+            __builtin_memcpy(to, u, 16);
         }
     }
-}
+};
 
 // ---- Few tokens: every token on its own.
 
@@ -122,22 +143,32 @@ template <typename X, typename W, int V, bool WHOLE> __global__ __launch_bounds_
     }
     __syncthreads();
     if (id < 0 || id >= a.count) return;
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = xs[wave][lane * 8 + i];
-    const int k = k0 + lane * 8;
+    constexpr int LANE = 16 / (int)sizeof(W), PIECES = 8 / LANE;
     const Matrix down(static_cast<const W *>(a.down) + (size_t)id * a.rank * a.K, a.rank, a.K, a.K, sizeof(W));
     const float alpha = a.alpha ? a.alpha[id] : 1.0f, col = a.col ? a.col[(size_t)blockIdx.y * a.N + n] : 1.0f;
-    W w[16][8];
     float s[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) weights<W, 8>(down, j0 + j < a.rank && k < a.K ? (uint32_t)(j0 + j) * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, k, a.K, WHOLE || k0 + kTokenRows <= a.K, w[j]);
+    for (int j = 0; j < 16; ++j) s[j] = 0.0f;
+    auto dots = [&](auto whole) {
+        W w[PIECES][16][LANE];
+        float x[PIECES][LANE];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        s[j] = 0.0f;
+        for (int p = 0; p < PIECES; ++p) {
+            const Cut<W, decltype(whole)::value> cut(k0 + lane * 8 + p * LANE, a.K);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[j] = __builtin_fmaf((float)w[j][i], x[i], s[j]);
-    }
+            for (int j = 0; j < 16; ++j) cut.load(down, j0 + j < a.rank ? (uint32_t)(j0 + j) * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, w[p][j]);
+#pragma unroll
+            for (int i = 0; i < LANE; ++i) x[p][i] = cut.keeps(i) ? xs[wave][cut.from - k0 + i] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+                for (int i = 0; i < LANE; ++i) s[j] = __builtin_fmaf((float)w[p][j][i], x[p][i], s[j]);
+    };
+    if (WHOLE || k0 + kTokenRows <= a.K) dots(std::true_type{});
+    else dots(std::false_type{});
     float sum[1];
     over_rows<16, 1, false>(s, lane, sum);
     if (stores<16, 1>(lane)) a.t[(((size_t)blockIdx.y * a.N + n) * a.parts + part) * ranks + j0 + column_of<16, 1>(lane)] = sum[0] * alpha * col;
@@ -200,7 +231,7 @@ template <typename C, typename W, int V> __device__ __forceinline__ void finish(
 constexpr int kExpandRows = 64, kExpandThreads = 1024, kExpandWaves = kExpandThreads / 64;
 
 template <typename C, typename W, int EACH, bool WHOLE> __global__ __launch_bounds__(kExpandThreads) void expand_tokens_kernel(const ExpandArgs a) {
-    constexpr int TOKENS = EACH * kExpandWaves;
+    constexpr int TOKENS = EACH * kExpandWaves, LANE = 16 / (int)sizeof(W), PIECES = 16 / LANE;
     constexpr bool SCALED = std::is_same<C, int32_t>::value;
     extern __shared__ __align__(16) float ts[];           // [token][rank]
     __shared__ float ys[kExpandRows * (TOKENS + 1)];      // [row][token]
@@ -234,14 +265,14 @@ template <typename C, typename W, int EACH, bool WHOLE> __global__ __launch_boun
         s[q] = id[q] >= 0 ? 0.0f : -0.0f;   // (what is added to nothing leaves it as it is)
     }
     for (int j0 = 0; j0 < a.rank; j0 += 16) {
-        W u[EACH][2][8];
+        W u[EACH][PIECES][LANE];
 #pragma unroll
         for (int q = 0; q < EACH; ++q)
             if (id[q] >= 0) {
                 const Matrix up(static_cast<const W *>(a.up) + (size_t)id[q] * a.M * a.rank, a.M, a.rank, a.rank, sizeof(W));
                 const uint32_t row_at = m0 + lane < a.M ? (uint32_t)(m0 + lane) * (uint32_t)a.rank * (uint32_t)sizeof(W) : kNowhere;
-                weights<W, 8>(up, row_at, j0, a.rank, WHOLE, u[q][0]);
-                weights<W, 8>(up, row_at, j0 + 8, a.rank, WHOLE, u[q][1]);
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) Cut<W, WHOLE>(j0 + p * LANE, a.rank).load(up, row_at, u[q][p]);
             }
         if (j0 == 0) {
             gather.finish(ts, ranks, gather.c);
@@ -251,7 +282,13 @@ template <typename C, typename W, int EACH, bool WHOLE> __global__ __launch_boun
         for (int q = 0; q < EACH; ++q)
             if (id[q] >= 0)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[q] = __builtin_fmaf((float)u[q][i / 8][i % 8], ts[(wave + q * kExpandWaves) * ranks + j0 + i], s[q]);
+                for (int p = 0; p < PIECES; ++p) {
+                    const Cut<W, WHOLE> cut(j0 + p * LANE, a.rank);
+                    if (!cut.any) continue;
+#pragma unroll
+                    for (int i = 0; i < LANE; ++i)
+                        if (cut.keeps(i)) s[q] = __builtin_fmaf((float)u[q][p][i], ts[(wave + q * kExpandWaves) * ranks + cut.from + i], s[q]);
+                }
     }
 #pragma unroll
     for (int q = 0; q < EACH; ++q) ys[lane * (TOKENS + 1) + wave + q * kExpandWaves] = s[q];
@@ -266,6 +303,105 @@ template <typename C, typename W, int EACH, bool WHOLE> __global__ __launch_boun
             finish<C, W, 1>(c1, col, SCALED && a.row ? a.row[m0 + row[o]] : 1.0f, add, y);
             store<W, 1>(Y, ((uint32_t)(m0 + row[o]) * (uint32_t)a.ldy + (uint32_t)(n0 + token[o])) * (uint32_t)sizeof(W), 0, 0, y);
         }
+}
+
+// ---- One token: one kernel.  Every workgroup works t out for itself, as that is a few reads of `down` from L2, and less than a second kernel has to wait.
+
+constexpr int kOneRank = 64, kOneSize = 1 << 16;   // most ranks; most elements of `down`
+constexpr int kOneRows = 64, kOneThreads = 1024, kOneShare = kOneThreads / kOneRows;   // kOneShare: threads of a row of Y
+
+struct OneArgs {
+    const void *X, *down, *up;
+    const int32_t *index;
+    const float *alpha;
+    const void *C;
+    void *Y;
+    const float *row, *col;
+    int32_t M, K, ldx, ldc, ldy, rank, count;
+};
+
+// x goes to LDS; then a wave does a row of `down` at a time, and 16 threads a row of `up`.
+template <typename X, typename C, typename W, bool WHOLE> __global__ __launch_bounds__(kOneThreads) void one_token_kernel(const OneArgs a) {
+    constexpr bool SCALED = std::is_same<C, int32_t>::value;
+    constexpr int LANE = 16 / (int)sizeof(W), WAVES = kOneThreads / 64, PIECE = 64 * LANE, AT_ONCE = 8;   // elements of a wave's load; loads on their way at a time
+    extern __shared__ __align__(16) float xs[];   // K, rounded up
+    __shared__ __align__(16) float ts[kOneRank];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int id = a.index[blockIdx.y];
+    const bool some = (uint32_t)id < (uint32_t)a.count;
+    const Matrix x(static_cast<const X *>(a.X) + (int64_t)blockIdx.y * a.K * a.ldx, a.K, 1, a.ldx, sizeof(X));
+    const Matrix from(static_cast<const C *>(a.C) + (int64_t)blockIdx.y * a.M * a.ldc, a.M, 1, a.ldc, sizeof(C));
+    const int row = t / kOneShare, p = t % kOneShare, m = (int)blockIdx.x * kOneRows + row;
+    C had[1];
+    load<C, 1>(from, m < a.M && p == 0 ? (uint32_t)m * (uint32_t)a.ldc * (uint32_t)sizeof(C) : kNowhere, 0, had);
+    float s = -0.0f;   // (what is added to nothing leaves it as it is)
+    if (some) {
+        for (int k = t; k < ((a.K + 7) & ~7); k += kOneThreads) {
+            X v[1];
+            load<X, 1>(x, k < a.K ? (uint32_t)k * (uint32_t)a.ldx * (uint32_t)sizeof(X) : kNowhere, 0, v);
+            xs[k] = (float)v[0];
+        }
+        const Matrix up(static_cast<const W *>(a.up) + (size_t)id * a.M * a.rank, a.M, a.rank, a.rank, sizeof(W));
+        const Matrix down(static_cast<const W *>(a.down) + (size_t)id * a.rank * a.K, a.rank, a.K, a.K, sizeof(W));
+        auto at_ranks = [&](auto what) {
+            if (a.rank % LANE == 0) what(Cut<W, true>(p * LANE, a.rank));
+            else what(Cut<W, false>(p * LANE, a.rank));
+        };
+        W u[LANE];
+        at_ranks([&](auto cut) { cut.load(up, m < a.M ? (uint32_t)m * (uint32_t)a.rank * (uint32_t)sizeof(W) : kNowhere, u); });
+        const float alpha = a.alpha ? a.alpha[id] : 1.0f;
+        auto at_piece = [&](int k, auto what) {   // (all but the last one of a row are whole)
+            if (WHOLE || k + PIECE <= a.K) what(Cut<W, true>(k + lane * LANE, a.K));
+            else what(Cut<W, false>(k + lane * LANE, a.K));
+        };
+        for (int j0 = 0; j0 < a.rank; j0 += WAVES) {
+            const int j = j0 + wave;
+            float dot = 0.0f;
+            for (int k0 = 0; k0 < a.K; k0 += PIECE * AT_ONCE) {
+                W w[AT_ONCE][LANE];
+#pragma unroll
+                for (int q = 0; q < AT_ONCE; ++q)
+                    if (k0 + q * PIECE < a.K) at_piece(k0 + q * PIECE, [&](auto cut) { cut.load(down, j < a.rank ? (uint32_t)j * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, w[q]); });
+                if (j0 == 0 && k0 == 0) __syncthreads();   // x is in LDS
+#pragma unroll
+                for (int q = 0; q < AT_ONCE; ++q)
+                    if (k0 + q * PIECE < a.K)
+                        at_piece(k0 + q * PIECE, [&](auto cut) {
+                            if (cut.any)
+#pragma unroll
+                                for (int i = 0; i < LANE; ++i) dot = __builtin_fmaf((float)w[q][i], cut.keeps(i) ? xs[cut.from + i] : 0.0f, dot);
+                        });
+            }
+            const float each[1] = {dot};
+            float sum[1];
+            over_rows<1, 1, false>(each, lane, sum);
+            if (lane == 0 && j < a.rank) ts[j] = sum[0] * alpha;
+        }
+        __syncthreads();
+        s = 0.0f;
+        at_ranks([&](auto cut) {
+            if (cut.any)
+#pragma unroll
+                for (int i = 0; i < LANE; ++i)
+                    if (cut.keeps(i)) s = __builtin_fmaf((float)u[i], ts[cut.from + i], s);
+        });
+        s += from_lane_xor<8>(s);
+        s += from_lane_xor<4>(s);
+        s += from_lane_xor<2>(s);
+        s += from_lane_xor<1>(s);
+    }
+    if (m >= a.M || p > 0) return;
+    float col[1] = {1.0f}, scale = 1.0f;
+    if constexpr (SCALED) {
+        if (a.col) col[0] = a.col[blockIdx.y];
+        if (a.row) scale = a.row[m];
+        if (some) s *= col[0];
+    }
+    const Matrix Y(static_cast<W *>(a.Y) + (int64_t)blockIdx.y * a.M * a.ldy, a.M, 1, a.ldy, sizeof(W));
+    const float c1[1] = {(float)had[0]}, add[1] = {s};
+    W y[1];
+    finish<C, W, 1>(c1, col, scale, add, y);
+    store<W, 1>(Y, (uint32_t)m * (uint32_t)a.ldy * (uint32_t)sizeof(W), 0, 0, y);
 }
 
 // ---- Many tokens: tiles of 64 on the matrix cores.
@@ -651,10 +787,11 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
 namespace {
 
 struct Plan {   // the kernels of a call, and what they go by
+    const void *one;   // one kernel, or
     const void *shrink, *expand;
     int parts, turns, slots, rows;
     int64_t shrink_grid, expand_grid;
-    int shrink_threads, expand_threads, expand_lds;
+    int shrink_threads, expand_threads, lds;
 };
 
 template <typename X, typename W, int RB> const void *shrink_tiles(bool whole) { return whole ? (const void *)shrink_tiles_kernel<X, W, RB, true> : (const void *)shrink_tiles_kernel<X, W, RB, false>; }
@@ -662,11 +799,21 @@ template <typename C, typename W, int RB> const void *expand_tiles(bool whole) {
 template <typename C, typename W, int EACH> const void *expand_tokens(bool whole) { return whole ? (const void *)expand_tokens_kernel<C, W, EACH, true> : (const void *)expand_tokens_kernel<C, W, EACH, false>; }
 template <typename X, typename W, int V> const void *shrink_tokens(bool whole) { return whole ? (const void *)shrink_tokens_kernel<X, W, V, true> : (const void *)shrink_tokens_kernel<X, W, V, false>; }
 
+template <typename X, typename C, typename W> const void *one_token(bool whole) { return whole ? (const void *)one_token_kernel<X, C, W, true> : (const void *)one_token_kernel<X, C, W, false>; }
+
 template <typename X, typename C, typename W> Plan plan_of(const sparsert_adapter_set &d) {
     Plan p{};
     constexpr int LANE = 16 / (int)sizeof(W);
     const bool whole_k = d.K % LANE == 0, whole_rank = d.rank % LANE == 0;
     const int ranks = (d.rank + 15) / 16 * 16;
+    // One token.  Measured as one kernel and as two, in us: K = 1024, ranks 8, 32, 64: half 3.6, 4.2, 5.7 and 5.6, 5.8, 6.3, binary32 3.6, 4.5, 6.0 and 5.7, 6.0, 6.6; K = 4096,
+    // rank 16: 4.7 and 6.0, 5.6 and 6.1, rank 32: 6.4 and 6.1, 7.9 and 6.4.  Odd K = 771, ranks 8, 32, 64: half 4.5, 6.0, 8.9 and 6.0, 6.2, 6.7, binary32 4.9, 7.1, 11.5 and 6.4, 6.7, 7.3.
+    if (d.N == 1 && d.rank <= kOneRank && (int64_t)ranks * d.K <= (whole_k ? kOneSize : kOneSize / 4)) {
+        p.one = one_token<X, C, W>(whole_k);
+        p.expand_grid = (d.M + kOneRows - 1) / kOneRows;
+        p.lds = (d.K + 7) / 8 * 8 * (int)sizeof(float);
+        return p;
+    }
     // Bytes of weights that the tokens read if every one reads its own: what the first kind of kernels spends its time on.
     const double own = (double)d.N * d.batch * ((double)d.M + d.K) * ranks * (int)sizeof(W);
     const double limit = (30e6 + 4e6 * std::min(d.count, kTile)) * (sizeof(W) == 4 ? 2 : 1);
@@ -698,7 +845,7 @@ template <typename X, typename C, typename W> Plan plan_of(const sparsert_adapte
     while (each > 1 && (blocks * (((int64_t)d.N + each * kExpandWaves - 1) / (each * kExpandWaves)) * d.batch < 256 || each * kExpandWaves * ranks > 8192)) each /= 2;   // (t of 32 KiB at most in LDS)
     p.expand = each == 4 ? expand_tokens<C, W, 4>(whole_rank) : each == 2 ? expand_tokens<C, W, 2>(whole_rank) : expand_tokens<C, W, 1>(whole_rank);
     p.expand_grid = ((int64_t)d.N + each * kExpandWaves - 1) / (each * kExpandWaves) * blocks; p.expand_threads = kExpandThreads;
-    p.expand_lds = each * kExpandWaves * ranks * (int)sizeof(float);
+    p.lds = each * kExpandWaves * ranks * (int)sizeof(float);
     return p;
 }
 
@@ -715,6 +862,10 @@ size_t adapters_workspace(const sparsert_adapter_set &d) { return (size_t)d.batc
 int launch_adapters(const AdaptersCall &c, std::string &err) {
     const sparsert_adapter_set &d = c.d;
     const Plan p = plan_of(d);
+    if (p.one) {
+        OneArgs a{c.X, c.down, c.up, c.index, c.alpha, c.C, c.Y, c.row, c.col, d.M, d.K, d.ldx, d.ldc, d.ldy, d.rank, d.count};
+        return launch_operator(p.one, dim3((uint32_t)p.expand_grid, (uint32_t)d.batch), kOneThreads, a, c.stream, err, p.lds);
+    }
     const auto whole = [](int64_t n) { return (n + 7) / 8 * 8; };
     if (int rc = check_launch(whole(p.shrink_grid), p.shrink_threads, err)) return rc;
     if (int rc = check_launch(whole(p.expand_grid), p.expand_threads, err)) return rc;
@@ -723,7 +874,7 @@ int launch_adapters(const AdaptersCall &c, std::string &err) {
     const auto grid = [&](int64_t n) { return dim3((uint32_t)whole(n), (uint32_t)d.batch); };
     if (int rc = launch_operator(p.shrink, grid(p.shrink_grid), p.shrink_threads, s, c.stream, err)) return rc;
     ExpandArgs e{c.C, c.up, c.index, c.row, c.col, t, c.Y, d.M, d.N, d.ldc, d.ldy, d.count, p.parts, p.rows, d.rank};
-    return launch_operator(p.expand, grid(p.expand_grid), p.expand_threads, e, c.stream, err, p.expand_lds);
+    return launch_operator(p.expand, grid(p.expand_grid), p.expand_threads, e, c.stream, err, p.lds);
 }
 
 }  // namespace sparsert

@@ -152,14 +152,16 @@ int sparsert_adapters(const sparsert_adapter_set *set, const void *X_dev, const 
         sparsert::AdaptersCall c{*set, X_dev, down_dev, up_dev, index_dev, alpha_dev, C_dev, row_scale_dev, col_scale_dev, Y_dev, workspace_dev, stream};
         sparsert_adapter_set &d = c.d;
         if (int rc = check_set(d)) return rc;
-        if (!X_dev || !down_dev || !up_dev || !index_dev || !C_dev || !Y_dev || !workspace_dev) return set_error(SPARSERT_EINVAL, "device pointer is NULL");
+        if (!X_dev || !down_dev || !up_dev || !index_dev || !C_dev || !Y_dev) return set_error(SPARSERT_EINVAL, "device pointer is NULL");
         if (misaligned(15, X_dev, down_dev, up_dev, C_dev, Y_dev, workspace_dev)) return set_error(SPARSERT_EINVAL, "matrices and workspace must be 16-byte aligned");
         if (misaligned(3, index_dev, alpha_dev, row_scale_dev, col_scale_dev)) return set_error(SPARSERT_EINVAL, "vectors must be 4-byte aligned");
         if (d.x_dtype != SPARSERT_I8 && (row_scale_dev || col_scale_dev)) return set_error(SPARSERT_EINVAL, "scales go with int8 X only");
         if (Y_dev == C_dev && (d.ldy != d.ldc || (d.x_dtype == SPARSERT_I8 && d.dtype != SPARSERT_F32)))
             return set_error(SPARSERT_EINVAL, "Y may be C only with elements of its size and at the same pitch");
         if (Y_dev == X_dev || workspace_dev == Y_dev) return set_error(SPARSERT_EINVAL, "Y overlaps X or the workspace");
-        if (workspace_bytes < sparsert::adapters_workspace(d)) return set_error(SPARSERT_EINVAL, "the workspace is smaller than sparsert_adapters_workspace says");
+        const size_t need = sparsert::adapters_workspace(d);
+        if (need && !workspace_dev) return set_error(SPARSERT_EINVAL, "workspace_dev is NULL");
+        if (workspace_bytes < need) return set_error(SPARSERT_EINVAL, "the workspace is smaller than sparsert_adapters_workspace says");
         if (int rc = check_stream(stream)) return rc;
         return sparsert::launch_adapters(c, err);
     });

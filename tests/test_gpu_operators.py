@@ -285,6 +285,74 @@ def test_adapters_of_real_sizes(M, K, N, rank, count, index, kind):
     assert call.read().tobytes() == y.tobytes()     # the same operands, the same bits
 
 
+# A single token is one kernel, without workspace, up to 65536 elements of an adapter's `down` (16384 where K is odd in its 16 bytes) and rank 64.
+@pytest.mark.parametrize("kind", ["f16", "f32", "i8f16", "i8f32"])
+@pytest.mark.parametrize("M,K,rank,batch", [
+    (64, 4096, 16, 1), (65, 4104, 16, 1), (63, 4095, 3, 2), (1, 1024, 64, 1), (129, 1023, 16, 3), (200, 1024, 63, 1), (200, 1023, 17, 1), (7, 600, 61, 1), (70, 7, 5, 4), (5, 3, 64, 1),
+    (1030, 256, 64, 1), (64, 256, 65, 1), (3, 1, 2, 70), (300, 12000, 4, 1), (90, 515, 33, 2)])
+def test_adapters_of_one_token(M, K, rank, batch, kind):
+    rng = np.random.default_rng(M + K + rank)
+    s = adapters_case(rng, M, K, 1, rank, 3, kind, batch)
+    s["index"][0] = 2
+    for pads in ((0, 0, 0), (6, 1, 3)):
+        call = AdaptersCall(s, pads=pads)
+        for _ in range(2):
+            call.run()
+            call.check(call.read())
+
+
+@pytest.mark.parametrize("kind", ["f16", "f32", "i8f32"])
+def test_one_token_is_computed_from_its_own_column_and_adapter_alone(kind):
+    rng = np.random.default_rng(5)
+    M, K, rank, batch = 70, 203, 13, 8
+    s = adapters_case(rng, M, K, 1, rank, 4, kind, batch)
+    s["index"][:, 0] = [0, 1, -1, 4, 0, np.iinfo(np.int32).min, 2, 0]
+    if kind != "i8f32":
+        s["x"][1, :, 0], s["x"][2, 5, 0], s["x"][3, K - 1, 0] = np.nan, np.nan, np.inf     # of token 1 alone; tokens 2 and 3 have no adapter
+    s["down"][2, rank - 1, K - 1], s["up"][2, M - 1, rank - 1] = np.inf, np.nan            # of token 6 alone
+    s["down"][3], s["up"][3] = np.nan, np.nan                                              # of none
+    sound = [0, 4, 7] + ([1] if kind == "i8f32" else [])
+    clean = {k: None if v is None else v.copy() for k, v in s.items()}
+    for k in ("x", "down", "up"):
+        clean[k] = np.where(np.isfinite(clean[k]), clean[k], 0).astype(clean[k].dtype)
+    got, want = (AdaptersCall(v, pads=(1, 1, 1)) for v in (s, clean))
+    got.run()
+    want.run()
+    a, b = got.read(), want.read()
+    want.check(b)
+    assert got.need == 0
+    assert np.array_equal(a[sound], b[sound]) and not np.isfinite(a[6]).all()
+    none = [2, 3, 5]
+    assert np.array_equal(a[none], b[none])
+    if kind != "i8f32":
+        assert np.array_equal(a[none], s["c"][none]) and not np.isfinite(a[1]).any()
+
+
+@pytest.mark.parametrize("kind", ["f16", "i8f32"])
+def test_one_token_needs_no_workspace_and_is_captured(kind):
+    s = adapters_case(np.random.default_rng(11), 130, 512, 1, 16, 3, kind, 2)
+    s["index"][:] = 1
+    call = AdaptersCall(s)
+    call.run()
+    y = call.read()
+    call.check(y)
+    v = call.v
+
+    def without():
+        sp.adapters(call.d, call.X.at, at(v["down"]), at(v["up"]), at(v["index"]), at(v["alpha"]), call.C.at, at(v["row"]), at(v["col"]), call.Y.at, 0, 0, stream())
+
+    without()
+    assert call.read().tobytes() == y.tobytes()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        without()
+    for i in range(3):
+        v["index"][0, 0] = i      # the graph reads what lies there when it runs
+        graph.replay()
+        s["index"][0, 0] = i
+        call.check(call.read())
+
+
 # Calls whose tokens would read more weights than their tiles of 64 share go to the matrix cores: over 34 MB with one adapter, 4 MB more for each other one, twice that in single precision.
 @pytest.mark.parametrize("kind", ["f16", "f32", "i8f16", "i8f32"])
 @pytest.mark.parametrize("M,K,N,rank,count,batch,index", [
