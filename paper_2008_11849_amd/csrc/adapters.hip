@@ -483,19 +483,20 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
 #pragma unroll
     for (int e = 0; e < Q::LANE; ++e)
         x_at[e] = tokens.columns.any ? ((uint32_t)(lane_row + e) * (uint32_t)a.ldx + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(X) : kNowhere;
-    auto fetch_x = [&](int turn, Loads &l) {
+    // (Every fetch is made, if of nothing: where one might be left out, the compiler has to wait for the whole of the one before it.)
+    auto fetch_x = [&](bool any, int turn, Loads &l) {
 #pragma unroll
-        for (int e = 0; e < Q::LANE; ++e) load<X, 4>(from, x_at[e], (uint32_t)turn * (uint32_t)TURN * (uint32_t)a.ldx * (uint32_t)sizeof(X), l.v[e]);
+        for (int e = 0; e < Q::LANE; ++e) load<X, 4>(from, any ? x_at[e] : kNowhere, (uint32_t)turn * (uint32_t)TURN * (uint32_t)a.ldx * (uint32_t)sizeof(X), l.v[e]);
     };
     auto fetch_w = [&](int id, int turn, Loads &l) {
-        const Matrix down(static_cast<const W *>(a.down) + (size_t)id * a.rank * a.K, a.rank, a.K, a.K, sizeof(W));
+        const Matrix down(id >= 0 ? static_cast<const W *>(a.down) + (size_t)id * a.rank * a.K : nullptr, a.rank, a.K, a.K, sizeof(W));
         const int k = turn * TURN + lane_row;
         if constexpr (WHOLE) {
             const uint32_t at = k < a.K ? ((uint32_t)i * (uint32_t)a.K + (uint32_t)lane_row) * (uint32_t)sizeof(W) : kNowhere;   // (ranks past the last lie outside, too)
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
                 W v[Q::LANE];
-                load<W, Q::LANE>(down, at + (k < a.K ? (uint32_t)(b * 16) * (uint32_t)a.K * (uint32_t)sizeof(W) : 0), (uint32_t)turn * (uint32_t)TURN * (uint32_t)sizeof(W), v);
+                load<W, Q::LANE>(down, at + (k < a.K ? (uint32_t)(b * 16) * (uint32_t)a.K * (uint32_t)sizeof(W) : 0), id >= 0 ? (uint32_t)turn * (uint32_t)TURN * (uint32_t)sizeof(W) : 0, v);
                 __builtin_memcpy(&l.w[b], v, 16);
             }
         } else {
@@ -506,7 +507,7 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
             }
         }
     };
-    fetch_x(first, even);
+    fetch_x(true, first, even);
     int left[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) left[c] = tokens.id[c];
@@ -537,13 +538,9 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
     // One turn; false when it was the last one.
     auto step = [&](Loads &now, Loads &ahead) {
         const bool done = turn + 1 == last;
-        if (!done) {
-            fetch_x(turn + 1, ahead);
-            fetch_w(id, turn + 1, ahead);
-        } else if (then >= 0) {
-            if (last - first > 1) fetch_x(first, ahead);
-            fetch_w(then, first, ahead);
-        }
+        const int of = done ? then : id, at = done ? first : turn + 1;
+        fetch_x(of >= 0 && last - first > 1, at, ahead);
+        fetch_w(of, at, ahead);
         if (fresh)
 #pragma unroll
             for (int c = 0; c < 4; ++c)
@@ -628,22 +625,26 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
         c_at[q] = any ? ((uint32_t)(g * 4 + q) * (uint32_t)a.ldc + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(C) : kNowhere;
         y_at[q] = any ? ((uint32_t)(g * 4 + q) * (uint32_t)a.ldy + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(W) : kNowhere;
     }
-    struct Block { C had[4][4]; float row[4]; frag w[RB]; };
+    constexpr bool TWO = RB < 4;   // (there are no registers for more)
+    struct Block { C had[4][4]; float row[4]; frag w[RB], w2[TWO ? RB : 1]; };   // weights of the first adapter of the tile; of the second one
+    // (Every fetch is made, if of nothing: where one might be left out, the compiler has to wait for the whole of the one before it.)
     auto fetch_c = [&](int m, Block &b) {
+        const bool some = m < end;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) load<C, 4>(from, c_at[q], (uint32_t)m * (uint32_t)a.ldc * (uint32_t)sizeof(C), b.had[q]);
+        for (int q = 0; q < 4; ++q) load<C, 4>(from, some ? c_at[q] : kNowhere, some ? (uint32_t)m * (uint32_t)a.ldc * (uint32_t)sizeof(C) : 0, b.had[q]);
         if constexpr (SCALED) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                float one[1] = {1.0f};
-                if (a.row) load<float, 1>(rows, (uint32_t)(g * 4 + q) * 4u, (uint32_t)m * 4u, one);
+                float one[1];
+                load<float, 1>(rows, some ? (uint32_t)(m + g * 4 + q) * 4u : kNowhere, 0, one);   // (0 where there are no scales)
                 b.row[q] = one[0];
             }
         }
     };
     auto up_of = [&](int m, int id, frag (&w)[RB]) {
-        const Matrix up(static_cast<const W *>(a.up) + (size_t)id * a.M * a.rank, a.M, a.rank, a.rank, sizeof(W));
-        const uint32_t block_at = (uint32_t)m * (uint32_t)a.rank * (uint32_t)sizeof(W);
+        const bool some = id >= 0 && m < end;
+        const Matrix up(some ? static_cast<const W *>(a.up) + (size_t)id * a.M * a.rank : nullptr, a.M, a.rank, a.rank, sizeof(W));
+        const uint32_t block_at = some ? (uint32_t)m * (uint32_t)a.rank * (uint32_t)sizeof(W) : 0;
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
             const int j = b * 16 + (HALF ? (g & 1) * 8 : g * 4);
@@ -653,7 +654,7 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
     };
     Block even, odd;
     const int mine = m0 + wave * 16;
-    if (mine < end) fetch_c(mine, even);
+    fetch_c(mine, even);
     int left[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) left[c] = tokens.id[c];
@@ -664,9 +665,11 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
     all = __all(all);
     auto fetch = [&](int m, Block &b) {
         fetch_c(m, b);
-        if (first >= 0) up_of(m, first, b.w);
+        up_of(m, first, b.w);
+        if constexpr (TWO) up_of(m, second, b.w2);
     };
-    if (first >= 0 && mine < end) up_of(mine, first, even.w);
+    up_of(mine, first, even.w);
+    if constexpr (TWO) up_of(mine, second, even.w2);
     // Row (n % 4) * 16 + n / 4 of ts is token n of the tile: the lanes of a quarter read rows that follow each other.
     auto row_of = [](int n) { return (n & 3) * 16 + (n >> 2); };
     float top = gather.finish(ts, PITCH, row_of(gather.c));
@@ -714,6 +717,7 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
     for (int b = 0; b < RB; ++b)
 #pragma unroll
         for (int c = 0; c < 4; ++c) x[b][c] = operands[b * 4 + c][lane];
+    const uint32_t ones = a.row ? 0u : __float_as_uint(1.0f);   // of rows without scales
     float col[4];
     if constexpr (SCALED) {
 #pragma unroll
@@ -721,45 +725,54 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
     }
     auto block = [&](int m, const Block &b) {
         float add[4][4];   // [row][token]
-        auto one = [&](int id, const frag (&w)[RB], bool every) {
+        // What an adapter adds to the tokens that are its own (alone: all are).
+        auto one = [&](int id, const frag (&w)[RB], auto alone) {
+            float4v acc[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const bool its = every || tokens.id[c] == id;
-                if (!every && !__any(its)) continue;
-                float4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int c = 0; c < 4; ++c) acc[c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int r = 0; r < RB; ++r) acc = Q::mma(w[r], x[r][c], acc);
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    // (In binary32 a product is worth a branch around it: 512 requests of a token each, 4096 rows, rank 16: 19 us for 25.  In half it is not.)
+                    if (!HALF && !decltype(alone)::value && !__any(tokens.id[c] == id)) continue;
+                    acc[c] = Q::mma(w[r], x[r][c], acc[c]);
+                }
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float v = HALF ? __builtin_ldexpf(acc[q], down[c]) : acc[q];
-                    add[q][c] = its ? v : add[q][c];
+                    const float v = HALF ? __builtin_ldexpf(acc[c][q], down[c]) : acc[c][q];
+                    add[q][c] = decltype(alone)::value || tokens.id[c] == id ? v : add[q][c];
                 }
-            }
         };
         if (all && first >= 0) {
-            one(first, b.w, true);
+            one(first, b.w, std::true_type{});
         } else {
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) add[q][c] = -0.0f;   // (what is added to nothing leaves it as it is)
             // (The next adapter's weights are on their way while one is multiplied.)
-            frag w[RB];
-            if (second >= 0) up_of(m, second, w);
-            if (first >= 0) one(first, b.w, false);
             int rest[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) rest[c] = left[c];
-            for (int id = second; id >= 0;) {
+            int id = TWO ? TileTokens::next(rest) : second;
+            frag w[RB];
+            up_of(m, id, w);
+            if (first >= 0) one(first, b.w, std::false_type{});
+            if constexpr (TWO)
+                if (second >= 0) one(second, b.w2, std::false_type{});
+            while (id >= 0) {
                 const int then = TileTokens::next(rest);
                 frag ahead[RB];
-                if (then >= 0) up_of(m, then, ahead);
-                one(id, w, false);
+                up_of(m, then, ahead);
+                one(id, w, std::false_type{});
                 id = then;
                 if (id < 0) break;
                 const int last = TileTokens::next(rest);
-                if (last >= 0) up_of(m, last, w);
-                one(id, ahead, false);
+                up_of(m, last, w);
+                one(id, ahead, std::false_type{});
                 id = last;
             }
         }
@@ -769,7 +782,7 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 float had = (float)b.had[q][c];
-                if constexpr (SCALED) had = had * col[c] * b.row[q];
+                if constexpr (SCALED) had = had * col[c] * __uint_as_float(__float_as_uint(b.row[q]) | ones);
                 y[c] = (W)(had + add[q][c]);
             }
             store<W, 4>(Y, y_at[q], (uint32_t)m * (uint32_t)a.ldy * (uint32_t)sizeof(W), any ? tokens.columns.skip : 0, y);
@@ -777,10 +790,11 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
     };
     constexpr int NEXT = WAVES * 16;
     for (int m = mine; m < end; m += 2 * NEXT) {
-        if (m + NEXT < end) fetch(m + NEXT, odd);
+        fetch(m + NEXT, odd);
         block(m, even);
-        if (m + 2 * NEXT < end) fetch(m + 2 * NEXT, even);
-        if (m + NEXT < end) block(m + NEXT, odd);
+        if (m + NEXT >= end) break;
+        fetch(m + 2 * NEXT, even);
+        block(m + NEXT, odd);
     }
 }
 
