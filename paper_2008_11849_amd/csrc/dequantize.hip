@@ -1,4 +1,7 @@
-// The int32 result of an int8 product times its row and column scales.
+// The int32 result of an int8 product times its row and column scales: y = c col row, in binary32, rounded once.
+//
+// Bound by memory: every element is read and written once.  4096 rows of 4093 in 4097, to binary32, 134 MB: 28.5 us, 4.7 TB/s, nine tenths of a large copy's rate (rows of odd pitch
+// begin anywhere: vectors are read and written wherever they lie).  768 x 1024 to half: 2.5 us, of which 1.7 are a kernel that does nothing.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -16,6 +19,7 @@ struct DequantArgs {
     int32_t M, N, ldc, ldy, passes;
 };
 
+// Strips as wide as the row allows, so that a wave reads a kilobyte of it at once.
 // A workgroup of 256 threads does a strip of V * L columns in `passes` * 256 / L rows: thread t has the V columns of lane t % L in the rows t / L, t / L +
 // 256 / L, ...  kDequantPasses rows are fetched before the first is scaled.
 constexpr int kDequantThreads = 256, kDequantPasses = 4;

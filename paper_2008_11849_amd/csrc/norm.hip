@@ -1,4 +1,11 @@
 // Root-mean-square norm over the features of every token, with the residual's addition and, for int8 products, quantisation.
+//
+// h = x + r,  v = h gamma,  f = 1 / sqrt(sum h^2 / K + eps),  y = v f.  int8: y = round(127 v / a) with a = max |v|, scale a f / 127: f drops out of
+// the integers, so that the sum of squares and the maximum come from one pass.  A token is a column: its sums run down the rows, lanes of a wave lie along them, so
+// that rows are read in runs, and columns meet in LDS.  Everything is held in binary32 and rounded once, at the stores; sums are added in one order, whatever the timing.
+//
+// Bounds: the wait for one read of memory and for two rounds through LDS in small calls (K = 1024, one token: 2.3 us, of which 1.7 are a kernel that does
+// nothing), memory in large ones: 4096 x 4096 half with both residuals, 134 MB: 33.6 us, 4.0 TB/s, where two copies of as many bytes take 28.2 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -102,7 +109,7 @@ template <typename T> __device__ __forceinline__ Matrix sum_of(const NormArgs &a
 template <typename Out> __device__ __forceinline__ Matrix result_of(const NormArgs &a) { return Matrix(static_cast<Out *>(a.Y) + (int64_t)blockIdx.y * a.K * a.ldy, a.K, a.N, a.ldy, sizeof(Out)); }
 
 // ---- One kernel: a workgroup of THREADS threads does a strip.  HELD: PASSES passes are all rows, and stay in registers between the
-// sums and the results; otherwise the rows are fetched twice.
+// sums and the results; otherwise the rows are fetched twice.  768 x 1024 half to int8: 5.0 us; 1027 x 771 of 784, binary32: 7.2 us.
 template <typename T, bool QUANT, int V, int L, int PASSES, bool HELD, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs a) {
     typedef out_t<T, QUANT> Out;
@@ -172,8 +179,8 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs a) {
     }
 }
 
-// ---- Two kernels, for columns too few and too long to fill the GPU: sums of every part of a strip, then the results.  A part is
-// `rows` rows of a strip.  The parts' sums and largest values lie in the caller's workspace, [batch][part][1 or 2][N].
+// ---- Two kernels, for columns too few and too long to fill the GPU, and for calls beyond the caches: sums of every part of a strip, then the results.  A part is
+// `rows` rows of a strip.  The second kernel reads the rows again, mostly from the caches.  The parts' sums and largest values lie in the caller's workspace, [batch][part][1 or 2][N].
 constexpr int kPartThreads = 256, kWideLanes = 16;
 constexpr int kPartPasses = 4;    // rows of a thread that are fetched at a time
 constexpr int kPartsAtOnce = 8;   // sums that a thread of the second kernel fetches at a time
@@ -223,6 +230,7 @@ template <typename T, bool QUANT, int V, int L> __global__ __launch_bounds__(kPa
     }
 }
 
+// FAR: H is not to be kept in the caches, so that it does not displace Y, which the next call reads first.
 template <typename T, bool QUANT, int V, int L, bool FAR> __global__ __launch_bounds__(kPartThreads) void norm_results_kernel(const NormArgs a) {
     typedef out_t<T, QUANT> Out;
     typedef Rows<T, V, L, kPartThreads> Part;
@@ -314,7 +322,8 @@ template <typename T, bool QUANT> const void *norm_of(const sparsert_norm &d, in
     return L == 8 ? norm_of<T, QUANT, W, 8>(d.K) : L == 4 ? norm_of<T, QUANT, W, 4>(d.K) : L == 2 ? norm_of<T, QUANT, W, 2>(d.K) : norm_of<T, QUANT, W, 1>(d.K);
 }
 
-// Estimate of a call as one kernel.
+// Estimate of a call as one kernel, fitted to calls of one to 4096 tokens of 768 to 8192 rows: a turn of the loads costs its wait and what the strip's narrowness wastes of
+// the lines that it touches.
 template <typename T> double one_kernel_us(const sparsert_norm &d, double bytes) {
     int V, L;
     strip_shape<T>(d, V, L);
@@ -339,8 +348,12 @@ template <typename T, bool QUANT, int V, int L, bool FAR = false> SplitNorm spli
 template <typename T, bool QUANT> SplitNorm split_of(const sparsert_norm &d) {
     constexpr int V = 16 / sizeof(T);
     const double bytes = (double)d.K * d.N * d.batch * (3 * sizeof(T) + sizeof(out_t<T, QUANT>));
+    // One kernel and two, measured in us (half): 1024 x 16 3.4 and 6.1, 768 x 1024 5.1 and 6.2, 2048 x 1024 10.3 and 7.7, 4096 x 128 12.9 and 6.5, 8192 x 1024
+    // 37 and 20.  Over 180 sizes the choices come to 0.6 % above the best of each.
     if (one_kernel_us<T>(d, bytes) <= (QUANT ? 6.2 : 5.3) + bytes / 4.4e6) return {};
     if (d.N < V) return d.N > 4 ? split_with<T, QUANT, 1, 8>(d, 256) : d.N > 2 ? split_with<T, QUANT, 1, 4>(d, 256) : split_with<T, QUANT, 1, 2>(d, 256);
+    // Strips of 8 vectors and of 16 (wide): 4096 x 1024 half 12.0 and 14.9, binary32 (67 MB) 19.2 and 18.1, 8192 x 1024 binary32 41 and 33, 4096 x 4096 half 44 and 34.
+    // H kept in the caches and not: 4096 x 4096 half 41.0 and 33.6, with a reader of Y and a later one of H behind it 72.5 and 69.2; 2048 x 4096 (67 MB) with the readers 37.0 and 38.4.
     constexpr int64_t wide = V * kWideLanes;
     if (bytes > 40e6 && d.batch * (d.N / wide) * (kPartThreads / wide * kPartsAtOnce) >= 256) return bytes > 100e6 ? split_with<T, QUANT, V, kWideLanes, true>(d, 512) : split_with<T, QUANT, V, kWideLanes>(d, 512);
     return d.N > 4 * V ? split_with<T, QUANT, V, 8>(d, 256) : d.N > 2 * V ? split_with<T, QUANT, V, 4>(d, 256)
