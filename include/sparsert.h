@@ -410,7 +410,7 @@ void sparsert_plan_destroy(sparsert_plan *plan);
  * borrowed and must not overlap what a call writes, except where an operator names a buffer that may be the same.  Columns behind
  * the N of a wider pitch are neither read nor written.
  * Errors: EINVAL (null or misaligned pointer, sizes that are not positive, a pitch under N, a type the operator does not
- * take, reserved fields set), EUNSUPPORTED (one matrix of a problem of 2 GiB and more; 2^28 rows or tokens and more; fewer tokens, but
+ * take, reserved fields set), EUNSUPPORTED (one matrix of a problem of 2 GiB and more; 2^28 rows or tokens and more; fewer, but
  * 2^22 at least, that need more workgroups than a launch can have), EHIP.
  */
 

@@ -886,6 +886,7 @@ int launch_adapters(const AdaptersCall &c, std::string &err) {
     const sparsert_adapter_set &d = c.d;
     const Plan p = plan_of(d);
     if (p.one) {
+        if (int rc = check_launch(p.expand_grid, kOneThreads, err)) return rc;
         OneArgs a{c.X, c.down, c.up, c.index, c.alpha, c.C, c.Y, c.row, c.col, d.M, d.K, d.ldx, d.ldc, d.ldy, d.rank, d.count};
         return launch_operator(p.one, dim3((uint32_t)p.expand_grid, (uint32_t)d.batch), kOneThreads, a, c.stream, err, p.lds);
     }

@@ -150,6 +150,7 @@ def test_more_workgroups_than_a_launch_can_have_are_refused():
     refused(sp.EUNSUPPORTED, "workgroups", sp.rms_norm, sp.RmsNorm(1, (1 << 28) - 1, dtype=sp.F32), P, 0, 0, 0, Q, 0, 0, 0)
     refused(sp.EUNSUPPORTED, "workgroups", sp.adapters, adapter_set(M=1, K=1, N=(1 << 28) - 1), P, P, P, P, 0, Q, 0, 0, S, T, 1 << 40)
     refused(sp.EUNSUPPORTED, "workgroups", sp.adapters, adapter_set(M=1, K=200, N=1 << 22, rank=256), P, P, P, P, 0, Q, 0, 0, S, T, 1 << 40)
+    refused(sp.EUNSUPPORTED, "workgroups", sp.adapters, adapter_set(M=(1 << 28) - 1, K=8, N=1, rank=1), P, P, P, P, 0, Q, 0, 0, S, 0, 0)
 
 
 @pytest.mark.parametrize("source", ["norm.hip", "dequantize.hip", "adapters.hip"])
