@@ -100,13 +100,14 @@ template <typename W, bool WHOLE> struct Cut {
                 to[i] = one[0];
             }
         }
-        if constexpr (!WHOLE) {
-            uint32_t u[4];
-            __builtin_memcpy(u, to, 16);
+        if constexpr (!WHOLE) mask(to);
+    }
+    __device__ __forceinline__ void mask(W (&to)[LANE]) const {
+        uint32_t u[4];
+        __builtin_memcpy(u, to, 16);
 #pragma unroll
-            for (int d = 0; d < 4; ++d) u[d] &= keep[d];
-            __builtin_memcpy(to, u, 16);
-        }
+        for (int d = 0; d < 4; ++d) u[d] &= keep[d];
+        __builtin_memcpy(to, u, 16);
     }
 };
 
@@ -489,7 +490,15 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
     for (int e = 0; e < Q::LANE; ++e)
         x_at[e] = tokens.columns.any ? ((uint32_t)(lane_row + e) * (uint32_t)a.ldx + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(X) : kNowhere;
     // (Every fetch is made, if of nothing: where one might be left out, the compiler has to wait for the whole of the one before it.)
+    // !WHOLE: how many rows up the piece begins that the end of K cuts short.
+    const int turns = (a.K + TURN - 1) / TURN, end_at = (turns - 1) * TURN + lane_row, up = !WHOLE && end_at < a.K ? max(0, end_at + Q::LANE - a.K) : 0;
     auto fetch_x = [&](bool any, int turn, Loads &l) {
+        if constexpr (!WHOLE) {   // (a first row of the turn, less those rows, may lie before it)
+            const uint32_t to = ((uint32_t)turn * (uint32_t)TURN - (turn + 1 == turns ? (uint32_t)up : 0u)) * (uint32_t)a.ldx * (uint32_t)sizeof(X);
+#pragma unroll
+            for (int e = 0; e < Q::LANE; ++e) load<X, 4>(from, any && tokens.columns.any ? x_at[e] + to : kNowhere, 0, l.v[e]);
+            return;
+        }
 #pragma unroll
         for (int e = 0; e < Q::LANE; ++e) load<X, 4>(from, any ? x_at[e] : kNowhere, (uint32_t)turn * (uint32_t)TURN * (uint32_t)a.ldx * (uint32_t)sizeof(X), l.v[e]);
     };
@@ -505,10 +514,13 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
                 __builtin_memcpy(&l.w[b], v, 16);
             }
         } else {
+            const Cut<W, false> cut(k, a.K);
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
-                const Piece<W> p = piece<W>(down, b * 16 + i < a.rank ? (uint32_t)(b * 16 + i) * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, 0, k, a.K, false);
-                __builtin_memcpy(&l.w[b], p.v, 16);
+                W v[Q::LANE];
+                load<W, Q::LANE>(down, cut.any && b * 16 + i < a.rank ? ((uint32_t)(b * 16 + i) * (uint32_t)a.K + (uint32_t)cut.from) * (uint32_t)sizeof(W) : kNowhere, 0, v);
+                cut.mask(v);
+                __builtin_memcpy(&l.w[b], v, 16);
             }
         }
     };
@@ -550,7 +562,7 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int e = 0; e < Q::LANE; ++e) x[c][e] = (W)now.v[e][c];
+                for (int e = 0; e < Q::LANE; ++e) x[c][e] = !WHOLE && e < up && turn + 1 == turns ? (W)0 : (W)now.v[e][c];
         fresh = last - first > 1;
 #pragma unroll
         for (int b = 0; b < RB; ++b)
@@ -843,7 +855,7 @@ template <typename X, typename C, typename W> Plan plan_of(const sparsert_adapte
     // (The tiles' lanes reckon with offsets of some rows on from any one.)
     const bool near = (int64_t)(kShrinkWaves * Step<W>::ROWS) * d.ldx * (int)sizeof(X) < 1ll << 31 && 16ll * std::max((int64_t)d.ldc * (int)sizeof(C), (int64_t)d.ldy * (int)sizeof(W)) < 1ll << 31 &&
                       64ll * d.K * (int)sizeof(W) < 1ll << 31 && 16ll * d.rank * (int)sizeof(W) < 1ll << 31;
-    if (near && d.N >= 4 && d.rank <= 64 && pieces_fit<W>(d.rank) && pieces_fit<W>(d.K) && own > limit) {
+    if (near && d.N >= 4 && d.rank <= 64 && pieces_fit<W>(d.rank) && d.K >= LANE && own > limit) {
         const int64_t tiles = ((int64_t)d.N + kTile - 1) / kTile;
         constexpr int TURN = kShrinkWaves * Step<W>::ROWS;
         const int turns = (d.K + TURN - 1) / TURN;
