@@ -109,7 +109,7 @@ template <typename T> __device__ __forceinline__ Matrix sum_of(const NormArgs &a
 template <typename Out> __device__ __forceinline__ Matrix result_of(const NormArgs &a) { return Matrix(static_cast<Out *>(a.Y) + (int64_t)blockIdx.y * a.K * a.ldy, a.K, a.N, a.ldy, sizeof(Out)); }
 
 // ---- One kernel: a workgroup of THREADS threads does a strip.  HELD: PASSES passes are all rows, and stay in registers between the
-// sums and the results; otherwise the rows are fetched twice.  768 x 1024 half to int8: 5.0 us; 4096 x 16: 6.4 us.
+// sums and the results; otherwise the rows are fetched twice.  768 x 1024 half to int8: 5.0 us; 4096 x 16: 5.8 us.
 template <typename T, bool QUANT, int V, int L, int PASSES, bool HELD, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs a) {
     typedef out_t<T, QUANT> Out;
@@ -302,7 +302,8 @@ template <typename T, bool QUANT, int V, int L> const void *norm_of(int K) {
     return (const void *)norm_kernel<T, QUANT, V, L, 4, false, kNormThreads>;
 }
 
-// Columns of a lane and lanes of a strip: 16 bytes, and as many lanes as leave 256 workgroups; narrower than that, one column to a lane.
+// Columns of a lane and lanes of a strip: 16 bytes, and as many lanes as leave 256 workgroups; narrower than that, one column to a lane.  Where a lane is a strip and 128 columns or
+// fewer are all, four columns in half, too: 4096 x 16 to int8 5.8 us, with eight 6.6; but 768 x 1024 5.6 and 5.0.
 template <typename T> void strip_shape(const sparsert_norm &d, int &V, int &L) {
     V = 16 / sizeof(T);
     if (d.N < V) {
@@ -312,6 +313,7 @@ template <typename T> void strip_shape(const sparsert_norm &d, int &V, int &L) {
     }
     const int64_t vectors = (int64_t)d.batch * ((d.N + V - 1) / V);
     L = vectors >= 8 * 256 ? 8 : vectors >= 4 * 256 ? 4 : vectors >= 2 * 256 ? 2 : 1;
+    if (L == 1 && (int64_t)d.batch * d.N <= 128) V = 4;
 }
 
 template <typename T, bool QUANT> const void *norm_of(const sparsert_norm &d, int &columns) {
@@ -320,6 +322,7 @@ template <typename T, bool QUANT> const void *norm_of(const sparsert_norm &d, in
     columns = V * L;
     if (V == 1) return L == 8 ? norm_of<T, QUANT, 1, 8>(d.K) : L == 4 ? norm_of<T, QUANT, 1, 4>(d.K) : L == 2 ? norm_of<T, QUANT, 1, 2>(d.K) : norm_of<T, QUANT, 1, 1>(d.K);
     constexpr int W = 16 / sizeof(T);
+    if (V == 4 && L == 1) return norm_of<T, QUANT, 4, 1>(d.K);
     return L == 8 ? norm_of<T, QUANT, W, 8>(d.K) : L == 4 ? norm_of<T, QUANT, W, 4>(d.K) : L == 2 ? norm_of<T, QUANT, W, 2>(d.K) : norm_of<T, QUANT, W, 1>(d.K);
 }
 
