@@ -6,7 +6,7 @@
 //
 // Bounds: 2 rank (M + K) operations a token are little beside C and Y of a prompt, or beside the adapters' weights of a few tokens; small calls are the wait for memory, twice
 // in each kernel.  One token, 1024 x 1024, rank 8: 3.5 us; 48 requests of 32 adapters, 4096 x 4096, rank 16: 8.7 us; 1024 tokens of prompts, 1024 -> 4096, rank 16: 11.0 us;
-// 2048 tokens of int8, 4096 x 4096, rank 64: 36.8 us, 2.1 TB/s.
+// 2048 tokens of int8, 4096 x 4096, rank 64: 37 us, 2.0 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
