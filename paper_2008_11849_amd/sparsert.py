@@ -335,7 +335,7 @@ class Adapters(_Descriptor):
         super().__init__(_AdapterSet(M, K, N, batch, rank, count, dtype, dtype if x_dtype is None else x_dtype, ldx, ldc, ldy))
 
     def workspace_bytes(self) -> int:
-        """Device memory that a call needs to work in; calls that may run at the same time need it each."""
+        """Device memory that a call needs to work in (0 = none); calls that may run at the same time need it each."""
         need = ctypes.c_size_t(0)
         _check(_lib.sparsert_adapters_workspace(self.handle, ctypes.byref(need)))
         return need.value
