@@ -541,8 +541,8 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
 #pragma unroll
         for (int c = 0; c < 4; ++c) ids[i * 4 + c] = tokens.id[c];
     // Thread t: two ranks of a token, the waves' sums in their order.
-    const int item = t >> 1, of_c = item >> 6, of_lane = item & 63, n = min(n0 + (of_lane & 15) * 4, a.N - 4) + of_c;
-    float *const to = a.t + (((size_t)blockIdx.y * a.N + n) * a.parts + part) * ranks + (of_lane >> 4) * 4 + (t & 1) * 2;
+    const int item = t >> 1, of_c = item >> 6, of_lane = item & 63, n = min(n0 + (of_lane & 15) * 4, a.N - 4) + of_c, of_j = (of_lane >> 4) * 4 + (t & 1) * 2;
+    float *const to = a.t + (((size_t)blockIdx.y * a.N + n) * a.parts + part) * ranks + of_j;
     const float col = a.col ? a.col[(size_t)blockIdx.y * a.N + n] : 1.0f;
     float4v acc[RB][4];
 #pragma unroll
@@ -593,8 +593,9 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
                     sum.x += u.x;
                     sum.y += u.y;
                 }
-                sum.x = sum.x * alpha * col;
-                sum.y = sum.y * alpha * col;
+                // (Ranks behind the last one are zeros, not what zeros for weights make of an infinite x: the second kernel multiplies them.)
+                sum.x = b * 16 + of_j < a.rank ? sum.x * alpha * col : 0.0f;
+                sum.y = b * 16 + of_j + 1 < a.rank ? sum.y * alpha * col : 0.0f;
                 if (b * 16 < ranks) *reinterpret_cast<float2 *>(to + b * 16) = sum;
             }
         }

@@ -637,3 +637,49 @@ def test_an_adapter_beyond_4_gib_of_weights():
     sp.adapters(a, at(X), at(down), at(up), at(I), 0, at(C), 0, 0, at(Y), at(ws), ws.numel(), stream())
     torch.cuda.synchronize()
     plain.check_adapters(Y.cpu().numpy(), s["x"], s["down"], s["up"], np.where(index == count - 1, 0, -1), None, s["c"], None, None)
+
+
+# ---------------------------------------------------------------- infinities are those of the formula, whichever kernels a call takes
+
+def column(s, n):
+    """Token n of a call in 64 bits, product by product: its result and the sum of the terms' sizes, [M] each."""
+    x, c = s["x"][0, :, n].astype(np.float64), s["c"][0, :, n].astype(np.float64)
+    if s["x"].dtype == np.int8:
+        x, c = x * float(s["col"][0, n]), c * s["row"].astype(np.float64) * float(s["col"][0, n])
+    a = s["index"][0, n]
+    if not 0 <= a < s["down"].shape[0]:
+        return c, np.abs(c)
+    down, up = s["down"][a].astype(np.float64), s["up"][a].astype(np.float64) * float(s["alpha"][a])
+    with np.errstate(invalid="ignore"):
+        return c + (up * (down * x).sum(axis=1)).sum(axis=1), np.abs(c) + (np.abs(up) * (np.abs(down * x)).sum(axis=1)).sum(axis=1)
+
+
+def check_columns(y, s, tokens):
+    K, rank = s["x"].shape[1], s["down"].shape[1]
+    for n in tokens:
+        want, size = column(s, n)
+        got, known = y[0, :, n].astype(np.float64), np.isfinite(want)
+        # (as in check_adapters: K and rank terms to a sum, factors and additions)
+        bound = size[known] * (K + rank + 16) * plain.U + plain.store_bound(want[known], y.dtype)
+        assert (np.abs(got[known] - want[known]) <= bound * 1.001).all(), n
+        assert np.array_equal(got[~known], want[~known], equal_nan=True), (n, got[~known], want[~known])
+
+
+# 3 and 40 tokens go one by one, 1100 in tiles on the matrix cores.
+@pytest.mark.parametrize("kind", ["f16", "f32"])
+@pytest.mark.parametrize("N", [1, 3, 40, 1100])
+@pytest.mark.parametrize("rank", [10, 20, 40])
+def test_infinite_activations_beside_fewer_ranks_than_a_block(rank, N, kind):
+    """Every t of the token is infinite; ranks that the adapter does not have are no terms."""
+    rng = np.random.default_rng(rank + N)
+    s = adapters_case(rng, 600, 512, N, rank, 2, kind)
+    s["down"], s["up"] = np.abs(s["down"]) + s["down"].dtype.type(0.01), np.abs(s["up"]) + s["up"].dtype.type(0.01)
+    s["index"][0, :] = np.arange(N) * 2 // N
+    hurt = sorted({0, N // 2, N - 1})
+    for i, n in enumerate(hurt):
+        s["x"][0, 100 + 50 * i, n] = (np.inf, -np.inf, np.inf)[i]
+    call = AdaptersCall(s)
+    call.run()
+    y = call.read()
+    assert np.isinf(y[0][:, hurt]).all()
+    check_columns(y, s, sorted({*hurt, *(n + 1 for n in hurt[:-1] if n + 1 < N)}))
