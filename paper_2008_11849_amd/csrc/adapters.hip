@@ -180,7 +180,7 @@ template <typename X, typename W, int V, bool WHOLE> __global__ __launch_bounds_
 }
 
 // t of up to TOKENS tokens from n0 on to LDS, rows of `pitch`: the parts added up in order.  THREADS / TOKENS threads share a token, each of them with four adjacent
-// ranks at a time, RANKS ranks in a turn.  Tokens without adapter get what happens to lie there.  Returns the largest |t| of this thread's.
+// ranks at a time, RANKS ranks in a turn.  Tokens without adapter get what happens to lie there.  Returns the largest finite |t| of this thread's.
 template <int THREADS, int RANKS, int TOKENS = 64> struct GatherT {
     static constexpr int SHARE = THREADS / TOKENS, AT_ONCE = 4, OWN = RANKS / (SHARE * 4);
     static_assert(RANKS % (SHARE * 4) == 0 && OWN >= 1, "whole turns");
@@ -197,6 +197,7 @@ template <int THREADS, int RANKS, int TOKENS = 64> struct GatherT {
                 u[p][i] = mine && p0 + p < parts && j < ranks ? from[((p0 + p) * ranks + j) / 4] : float4{0.0f, 0.0f, 0.0f, 0.0f};
             }
     }
+    static __device__ __forceinline__ float finite(float v) { return fabsf(v) < INFINITY ? fabsf(v) : 0.0f; }
     // Sends for the first of it.
     __device__ __forceinline__ GatherT(const ExpandArgs &a, int n0, int tokens) : parts(a.parts), ranks(ranks16(a.rank)), c((int)threadIdx.x / SHARE), share((int)threadIdx.x % SHARE), mine(c < tokens) {
         from = reinterpret_cast<const float4 *>(a.t + ((size_t)blockIdx.y * a.N + n0 + c) * parts * ranks);
@@ -219,7 +220,7 @@ template <int THREADS, int RANKS, int TOKENS = 64> struct GatherT {
             for (int i = 0; i < OWN; ++i) {
                 const int j = j0 + (share + i * SHARE) * 4;
                 if (mine && j < ranks) *reinterpret_cast<float4 *>(ts + row * pitch + j) = s[i];
-                top = larger(larger(larger(fabsf(s[i].x), fabsf(s[i].y)), larger(fabsf(s[i].z), fabsf(s[i].w))), top);
+                top = fmaxf(fmaxf(fmaxf(finite(s[i].x), finite(s[i].y)), fmaxf(finite(s[i].z), finite(s[i].w))), top);
             }
         }
         return top;
@@ -616,8 +617,8 @@ template <int RB> constexpr int kExpandTileWaves = RB < 4 ? 4 : 8;
 // A workgroup does 64 tokens and `rows` rows of Y (a multiple of 64), its waves 16 of them at a time; what such a block needs from memory is fetched while the one before it
 // is computed.
 // half: t is split into two halves, t = hi + lo, which the instruction's 32 steps take side by side for 16 ranks, beside the same 16 weights
-// twice: 22 bits of t, at a sixteenth of what binary32 instructions cost.  Every token's t is scaled by a power of two first, its largest
-// to 2^14 ... 2^15, so that neither half leaves its range: what lo loses below 2^-24 is 2^-39 of that largest.
+// twice: 22 bits of t, at a sixteenth of what binary32 instructions cost.  Every token's t is scaled by a power of two first, its largest finite one
+// to 2^14 ... 2^15, so that neither half leaves its range: what lo loses below 2^-24 is 2^-39 of that largest.  (An infinite t stays one, and has no lo.)
 template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds__(kExpandTileWaves<RB> * 64, RB < 2 ? 3 : 2) void expand_tiles_kernel(const ExpandArgs a) {
     constexpr bool SCALED = std::is_same<C, int32_t>::value, HALF = std::is_same<W, _Float16>::value;
     typedef Step<W> Q;
@@ -694,10 +695,10 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
     auto row_of = [](int n) { return (n & 3) * 16 + (n >> 2); };
     float top = gather.finish(ts, PITCH, row_of(gather.c));
     if constexpr (HALF) {
-        top = larger(top, from_lane_xor<1>(top));
-        top = larger(top, from_lane_xor<2>(top));
-        if constexpr (SHARE == 8) top = larger(top, from_lane_xor<4>(top));
-        if (t % SHARE == 0) exponents[t / SHARE] = top > 0.0f && top < INFINITY ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
+        top = fmaxf(top, from_lane_xor<1>(top));
+        top = fmaxf(top, from_lane_xor<2>(top));
+        if constexpr (SHARE == 8) top = fmaxf(top, from_lane_xor<4>(top));
+        if (t % SHARE == 0) exponents[t / SHARE] = top > 0.0f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
     }
     __syncthreads();
     // The second operand of every instruction, one for each 16 ranks and each quarter of the tokens: a wave makes some of a quarter.

@@ -683,3 +683,36 @@ def test_infinite_activations_beside_fewer_ranks_than_a_block(rank, N, kind):
     y = call.read()
     assert np.isinf(y[0][:, hurt]).all()
     check_columns(y, s, sorted({*hurt, *(n + 1 for n in hurt[:-1] if n + 1 < N)}))
+
+
+def selecting(s, rng):
+    """Makes t_j of adapter a the token's x in row 3 j + a, as it is."""
+    s["down"][:] = 0
+    for a in range(s["down"].shape[0]):
+        for j in range(s["down"].shape[1]):
+            s["down"][a, j, 3 * j + a] = 1
+
+
+@pytest.mark.parametrize("kind", ["f16", "i8f16", "f32"])
+@pytest.mark.parametrize("N", [1, 3, 40, 1100])
+@pytest.mark.parametrize("rank", [8, 24, 64])
+def test_an_infinite_inner_value_beside_large_ones(rank, N, kind):
+    """One t is infinite; the others, beyond half's range and of the other sign, are finite."""
+    rng = np.random.default_rng(rank + N)
+    s = adapters_case(rng, 600, 512, N, rank, 2, kind)
+    selecting(s, rng)
+    s["index"][0, :] = np.arange(N) * 2 // N
+    w = s["down"].dtype.type
+    s["down"][:, 0, :2], s["down"][0, 1, 3], s["down"][1, 1, 4] = 0, 60000, 60000
+    s["down"][:, 0, 2] = np.inf
+    s["x"][0, 2, :] = np.where(np.arange(N) % 2, 1, -1)
+    s["x"][0, 3:5, :] = np.where(np.arange(N) % 2, 50, -50)
+    if s["col"] is not None:
+        s["col"][:] = 0.5
+    s["up"] = (np.abs(s["up"]) * w(0.01) + w(0.001)) * np.where(np.arange(rank) == 0, 1, -1).astype(w)
+    assert abs(column(s, 0)[1]).max() == np.inf
+    call = AdaptersCall(s)
+    call.run()
+    y = call.read()
+    assert np.isinf(y).all()
+    check_columns(y, s, sorted({0, N // 3, N // 2, N - 1}))
