@@ -797,6 +797,31 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
                 id = last;
             }
         }
+        if constexpr (HALF) {
+            // Halves of t say nothing about infinities: an infinite weight times lo is undefined or of any sign.  Sums that are not finite are made again from t itself.
+            float most = 0.0f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) most = __builtin_elementwise_maximum(most, fabsf(add[q][c]));   // (undefined if one is)
+            if (__builtin_expect(__any(!(most < INFINITY)), 0)) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (!(fabsf(add[q][c]) < INFINITY)) {
+                            int of = tokens.id[c], n = tokens.columns.first + c - n0, at = m + g * 4 + q;
+                            asm volatile("" : "+v"(of), "+v"(n), "+v"(at));   // (or the addresses of all sixteen are reckoned ahead and fill the registers)
+                            if (of < 0 || at >= a.M) continue;
+                            const W *const up = static_cast<const W *>(a.up) + ((size_t)of * a.M + at) * a.rank;
+                            const float *const from = ts + row_of(n) * PITCH;
+                            float s = 0.0f;
+#pragma unroll 1
+                            for (int j = 0; j < a.rank; ++j) s = __builtin_fmaf((float)up[j], from[j], s);
+                            add[q][c] = s;
+                        }
+            }
+        }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             W y[4];

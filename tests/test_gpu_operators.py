@@ -716,3 +716,34 @@ def test_an_infinite_inner_value_beside_large_ones(rank, N, kind):
     y = call.read()
     assert np.isinf(y).all()
     check_columns(y, s, sorted({0, N // 3, N // 2, N - 1}))
+
+
+@pytest.mark.parametrize("kind", ["f16", "i8f16", "f32", "i8f32"])
+@pytest.mark.parametrize("N", [1, 3, 40, 1100])
+@pytest.mark.parametrize("rank", [8, 24, 64])
+def test_infinite_weights_of_up(rank, N, kind):
+    """Whatever t they meet: one that half holds, ones that it rounds up and down, one far under the token's largest, none."""
+    rng = np.random.default_rng(rank + N)
+    M = 600
+    s = adapters_case(rng, M, 512, N, rank, 2, kind)
+    selecting(s, rng)
+    s["index"][0, :] = np.arange(N) * 2 // N
+    s["alpha"][:] = 1.0
+    special = [1.0, 0.3, -0.7, 0.0, 2.0 ** -24] if s["x"].dtype != np.int8 else [100, 33, -77, 0, 1]
+    rows, j = [0, 17, 18, M - 1], rank - 2
+    hurt = [n for n in (0, 1, 2, N // 2, N // 2 + 1, N // 2 + 2, N - 3, N - 2, N - 1) if 0 <= n < N]
+    for i, n in enumerate(hurt):
+        a = s["index"][0, n]
+        s["x"][0, 3 * j + a, n] = special[(i + rank // 8 + N) % 5]
+        if s["x"].dtype != np.int8 and i % 2:
+            s["x"][0, a, n] = 60000.0          # the token's largest
+    s["up"][:, :, 0] *= s["up"].dtype.type(1e-3)
+    s["up"][:, rows[:3], j] = np.array([np.inf, -np.inf, np.inf])
+    s["up"][:, rows[2], j + 1] = -np.inf
+    s["up"][1, rows[3], j] = np.inf
+    call = AdaptersCall(s)
+    call.run()
+    y = call.read()
+    check_columns(y, s, sorted({*hurt, N // 3}))
+    others = np.delete(np.arange(M), rows)
+    plain.check_adapters(y[:, others], s["x"], s["down"], s["up"][:, others], s["index"], s["alpha"], s["c"][:, others], None if s["row"] is None else s["row"][others], s["col"])
