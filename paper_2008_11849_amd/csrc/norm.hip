@@ -29,9 +29,15 @@ struct NormArgs {
     int32_t parts, rows;   // parts of a column, and rows of each
 };
 
+// 1 / sqrt(m), rounded once: a root and a quotient are two roundings, 1.5 times as far off.  A step of Newton's from there, on what is left of m r r to 1, exactly.
+__device__ __forceinline__ float reciprocal_root(float m) {
+    const float r = 1.0f / sqrtf(m), h = m * r, rest = __builtin_fmaf(-h, r, 1.0f) - __builtin_fmaf(m, r, -h) * r;
+    return r > 0.0f ? __builtin_fmaf(0.5f * r, rest, r) : r;   // (of infinity it is 0)
+}
+
 // What a column's weighted sums are multiplied with, from the sum of its squares and its largest |h * gamma|.
 template <bool QUANT> __device__ __forceinline__ float factor_of(float total, float most, const NormArgs &a, float &scale) {
-    const float inv = 1.0f / sqrtf(total / (float)a.K + a.eps);
+    const float inv = reciprocal_root(total / (float)a.K + a.eps);
     if constexpr (!QUANT) return inv;
     const bool sound = total < INFINITY && most < INFINITY, some = most >= 0x1p-100f;
     scale = !sound ? NAN : some ? most * inv / 127.0f : 0.0f;

@@ -747,3 +747,14 @@ def test_infinite_weights_of_up(rank, N, kind):
     check_columns(y, s, sorted({*hurt, N // 3}))
     others = np.delete(np.arange(M), rows)
     plain.check_adapters(y[:, others], s["x"], s["down"], s["up"][:, others], s["index"], s["alpha"], s["c"][:, others], None if s["row"] is None else s["row"][others], s["col"])
+
+
+@pytest.mark.parametrize("K,N", [(2, 4000), (8192, 256), (8192, 3)])
+def test_norm_factor_is_rounded_once(K, N, way):
+    """Columns of a one, whose result is the factor, and a number that makes the mean of the squares exact; eps is lost beside it."""
+    x = np.zeros((1, K, N), dtype=np.float32)
+    x[0, 0, :], x[0, K - 1, :] = 1, np.arange(1, N + 1) / 64
+    y, _, _ = run_norm(way, x, None, None, np.float32, eps=1e-30)
+    want = 1 / np.sqrt((1 + x[0, K - 1, :].astype(np.float64) ** 2) / K)
+    # one rounding; what is behind it is of the order of its square
+    assert (np.abs(y[0, 0, :] - want) <= want * plain.U * (1 + 2.0 ** -20)).all()
