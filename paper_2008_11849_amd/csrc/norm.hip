@@ -326,8 +326,10 @@ template <typename T, bool QUANT> const void *norm_of(const sparsert_norm &d, in
     int V, L;
     strip_shape<T>(d, V, L);
     columns = V * L;
-    if (V == 1) return L == 8 ? norm_of<T, QUANT, 1, 8>(d.K) : L == 4 ? norm_of<T, QUANT, 1, 4>(d.K) : L == 2 ? norm_of<T, QUANT, 1, 2>(d.K) : norm_of<T, QUANT, 1, 1>(d.K);
     constexpr int W = 16 / sizeof(T);
+    if constexpr (W > 4)   // (single columns are fewer than W)
+        if (V == 1 && L == 8) return norm_of<T, QUANT, 1, 8>(d.K);
+    if (V == 1) return L == 4 ? norm_of<T, QUANT, 1, 4>(d.K) : L == 2 ? norm_of<T, QUANT, 1, 2>(d.K) : norm_of<T, QUANT, 1, 1>(d.K);
     if (V == 4 && L == 1) return norm_of<T, QUANT, 4, 1>(d.K);
     return L == 8 ? norm_of<T, QUANT, W, 8>(d.K) : L == 4 ? norm_of<T, QUANT, W, 4>(d.K) : L == 2 ? norm_of<T, QUANT, W, 2>(d.K) : norm_of<T, QUANT, W, 1>(d.K);
 }
@@ -361,7 +363,9 @@ template <typename T, bool QUANT> SplitNorm split_of(const sparsert_norm &d) {
     // One kernel and two, measured in us (half): 1024 x 16 3.4 and 6.1, 768 x 1024 5.1 and 6.2, 2048 x 1024 10.3 and 7.7, 4096 x 128 12.9 and 6.5, 8192 x 1024
     // 37 and 20.  Over 180 sizes the choices come to 0.6 % above the best of each.
     if (one_kernel_us<T>(d, bytes) <= (QUANT ? 6.2 : 5.3) + bytes / 4.4e6) return {};
-    if (d.N < V) return d.N > 4 ? split_with<T, QUANT, 1, 8>(d, 256) : d.N > 2 ? split_with<T, QUANT, 1, 4>(d, 256) : split_with<T, QUANT, 1, 2>(d, 256);
+    if constexpr (V > 4)
+        if (d.N > 4 && d.N < V) return split_with<T, QUANT, 1, 8>(d, 256);
+    if (d.N < V) return d.N > 2 ? split_with<T, QUANT, 1, 4>(d, 256) : split_with<T, QUANT, 1, 2>(d, 256);
     // Strips of 8 vectors and of 16 (wide): 4096 x 1024 half 12.0 and 14.9, binary32 (67 MB) 19.2 and 18.1, 8192 x 1024 binary32 41 and 33, 4096 x 4096 half 44 and 34.
     // H kept in the caches and not: 4096 x 4096 half 41.0 and 33.6, with a reader of Y and a later one of H behind it 72.5 and 69.2; 2048 x 4096 (67 MB) with the readers 37.0 and 38.4.
     constexpr int64_t wide = V * kWideLanes;
