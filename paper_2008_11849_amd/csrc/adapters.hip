@@ -594,9 +594,14 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
                     sum.x += u.x;
                     sum.y += u.y;
                 }
-                // (Ranks behind the last one are zeros, not what zeros for weights make of an infinite x: the second kernel multiplies them.)
-                sum.x = b * 16 + of_j < a.rank ? sum.x * alpha * col : 0.0f;
-                sum.y = b * 16 + of_j + 1 < a.rank ? sum.y * alpha * col : 0.0f;
+                sum.x = sum.x * alpha * col;
+                sum.y = sum.y * alpha * col;
+                if constexpr (std::is_same<W, float>::value) {
+                    // Ranks behind the last one are zeros, not what zeros for weights make of an infinite x: the second kernel multiplies them.  (For half it
+                    // makes sums that are not finite again, of the ranks there are.)
+                    if (b * 16 + of_j >= a.rank) sum.x = 0.0f;
+                    if (b * 16 + of_j + 1 >= a.rank) sum.y = 0.0f;
+                }
                 if (b * 16 < ranks) *reinterpret_cast<float2 *>(to + b * 16) = sum;
             }
         }
