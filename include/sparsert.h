@@ -495,10 +495,15 @@ typedef struct sparsert_adapter_set {
  *
  * where x = X and c = C or, for int8 X, x[k,n] = X[k,n] * col_scale[n] and c[m,n] = C[m,n] * col_scale[n] * row_scale[m]:
  * the call is then given what sparsert_spmm was given and what it wrote, and takes sparsert_dequantize's place.
- * Sums are binary32 and Y is rounded once.  alpha[a] * t is kept in binary32, or, for many tokens of half weights, in two halves: off by 2^-22
- * of itself or by 2^-39 of the token's largest, whichever is more.  (A weight of `up` that is large where t is under 2^-17 of that largest, in a row that is zero
- * where t is large, meets fewer bits than binary32 has.)  Infinite and undefined results are those of the formula, with t in binary32, whichever way a call takes.  A token is
- * computed from its own column and adapter alone: what is infinite or undefined elsewhere does not reach it.
+ * Sums are binary32 and Y is rounded once.  alpha[a] * t is kept in binary32, or, for many tokens of half weights, in two
+ * halves: off by 2^-22 of itself or by 2^-39 of the token's largest, whichever is more.  (So a t under 2^-17 of that largest has
+ * fewer bits than 22, which shows in rows of `up` that are zero where t is large, and large where it is small.)
+ * Infinities and undefined values in X, C, the weights and alpha make of a result what the formula makes of it with t in binary32;
+ * col_scale is applied to t or to the sum over t.  A token is computed from its own column and adapter alone:
+ * what is infinite or undefined elsewhere does not reach it.
+ *
+ * Many tokens are fast with ranks up to 64, in half even ones and those from 8 on: an adapter is read once for 64 tokens.  Of other
+ * ranks every token reads its own (half, 4096 x 4096, 2048 tokens: rank 64 37 us, rank 65 601 us).
  *
  *   X_dev          [batch, K, ldx]
  *   down_dev       [count, rank, K], up_dev [count, M, rank]

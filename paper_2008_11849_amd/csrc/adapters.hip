@@ -4,9 +4,9 @@
 // t lies in the caller's workspace, [batch * N][part][ranks, rounded up to 16], in binary32.  (The factors are in t, so that the second kernel
 // fetches everything but `up` without waiting for an index.)
 //
-// Bounds: 2 rank (M + K) operations a token are little beside C and Y of a prompt, or beside the adapters' weights of a few tokens; small calls are the wait for memory, twice
-// in each kernel.  One token, 1024 x 1024, rank 8: 3.5 us; 48 requests of 32 adapters, 4096 x 4096, rank 16: 8.7 us; 1024 tokens of prompts, 1024 -> 4096, rank 16: 11.0 us;
-// 2048 tokens of int8, 4096 x 4096, rank 64: 37 us, 2.0 TB/s.
+// Bounds: 2 rank (M + K) operations a token are little beside C and Y of a prompt, or beside the adapters' weights of a few tokens; small calls are
+// the wait for memory, twice in each kernel.  One token, 1024 x 1024, rank 8: 3.5 us; 48 requests of 32 adapters, 4096 x 4096, rank 16: 8.6 us;
+// 1024 tokens of prompts, 1024 -> 4096, rank 16: 11.2 us; 2048 tokens of int8, 4096 x 4096, rank 64: 37 us, 2.0 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -40,9 +40,10 @@ struct ExpandArgs {
 
 __device__ __forceinline__ int ranks16(int rank) { return (rank + 15) & ~15; }
 
-// 16 bytes of weights of a row of `end` elements, from element `at` on; zeros for those behind the row's end.  (There lies the next row, which may hold
-// infinities: it has to be left out, not multiplied by zero.)  `whole`: no piece is cut short by the end.  A piece that is reads the row's last 16 bytes and moves
-// them down.  A row shorter than that is read over its end, so it has an even number of halves: a range is checked in steps of four bytes.
+// 16 bytes of weights of a row of `end` elements, from element `at` on; zeros for those behind the row's end.  (There lies the next row, which may
+// hold infinities: it has to be left out, not multiplied by zero.)  `whole`: no piece is cut short by the end.  A piece that is reads the row's
+// last 16 bytes and moves them down.  A row shorter than that is read over its end, so it has an even number of halves: a range is checked in steps
+// of four bytes.
 template <typename W> struct Piece { W v[16 / sizeof(W)]; };
 template <typename W> __device__ __forceinline__ Piece<W> piece(const Matrix &m, uint32_t row_at, uint32_t common, int at, int end, bool whole) {
     constexpr int LANE = 16 / sizeof(W), BITS = 8 * sizeof(W);
@@ -70,8 +71,9 @@ template <typename W> __device__ __forceinline__ Piece<W> piece(const Matrix &m,
 // Can rows of `end` elements be read so?
 template <typename W> bool pieces_fit(int end) { return end >= 16 / (int)sizeof(W) || end * sizeof(W) % 4 == 0; }
 
-// The same for the kernels that multiply a lane's piece of many rows with numbers of its own: a piece that the end cuts short is the row's last 16 bytes as they
-// lie, without what belongs to the lane before, and the lane moves its numbers instead (2.6 us less than moving the weights, for 16 rows of half weights).
+// The same for the kernels that multiply a lane's piece of many rows with numbers of its own: a piece that the end cuts short is the row's last 16
+// bytes as they lie, without what belongs to the lane before, and the lane moves its numbers instead (2.6 us less than moving the weights, for 16
+// rows of half weights).
 template <typename W, bool WHOLE> struct Cut {
     static constexpr int LANE = 16 / sizeof(W), EACH = 4 / sizeof(W);
     int from, end;
@@ -115,13 +117,14 @@ template <typename W, bool WHOLE> struct Cut {
 
 constexpr int kTokenGroup = 8, kTokenRows = 512, kTokenThreads = 512;   // tokens and rows of x of a workgroup; a wave for each token
 
-// The group's x goes to LDS once, whole rows of eight tokens at a time (V = 8; 1: fewer than eight tokens); then wave w has token w, and its lane l the rows 8 l ... 8 l + 7,
-// which it multiplies with 16 rows of `down`; other workgroups have the others.
+// The group's x goes to LDS once, whole rows of eight tokens at a time (V = 8; 1: fewer than eight tokens); then wave w has token w, and its lane l
+// the rows 8 l ... 8 l + 7, which it multiplies with 16 rows of `down`; other workgroups have the others.
 template <typename X, typename W, int V, bool WHOLE> __global__ __launch_bounds__(kTokenThreads) void shrink_tokens_kernel(const ShrinkArgs a) {
     __shared__ __align__(16) float xs[kTokenGroup][kTokenRows + 4];
     const int groups = (a.N + kTokenGroup - 1) / kTokenGroup, ranks = ranks16(a.rank), blocks = ranks / 16;
     if ((int)blockIdx.x >= groups * a.parts * blocks) return;
-    const int group = blockIdx.x % groups, part = blockIdx.x / groups % a.parts, j0 = blockIdx.x / groups / a.parts * 16, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int group = blockIdx.x % groups, part = blockIdx.x / groups % a.parts, j0 = blockIdx.x / groups / a.parts * 16, t = threadIdx.x,
+        lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int n0 = group * kTokenGroup, k0 = part * kTokenRows, n = n0 + wave;
     const int id = n < a.N ? a.index[(size_t)blockIdx.y * a.N + n] : -1;
     {
@@ -133,7 +136,8 @@ template <typename X, typename W, int V, bool WHOLE> __global__ __launch_bounds_
 #pragma unroll
             for (int p = 0; p < V / PIECE; ++p) {
                 X v[PIECE];
-                load<X, PIECE>(x, k < a.K ? ((uint32_t)k * (uint32_t)a.ldx + (uint32_t)(columns.first + p * PIECE)) * (uint32_t)sizeof(X) : kNowhere, 0, v);
+                load<X, PIECE>(x, k < a.K ? ((uint32_t)k * (uint32_t)a.ldx + (uint32_t)(columns.first + p * PIECE)) * (uint32_t)sizeof(X) : kNowhere,
+                               0, v);
 #pragma unroll
                 for (int i = 0; i < PIECE; ++i)
                     if (p * PIECE + i >= columns.skip) xs[p * PIECE + i - columns.skip][t] = (float)v[i];
@@ -161,7 +165,8 @@ template <typename X, typename W, int V, bool WHOLE> __global__ __launch_bounds_
         for (int p = 0; p < PIECES; ++p) {
             const Cut<W, decltype(whole)::value> cut(k0 + lane * 8 + p * LANE, a.K);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) cut.load(down, j0 + j < a.rank ? (uint32_t)(j0 + j) * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, w[p][j]);
+            for (int j = 0; j < 16; ++j)
+                cut.load(down, j0 + j < a.rank ? (uint32_t)(j0 + j) * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, w[p][j]);
 #pragma unroll
             for (int i = 0; i < LANE; ++i) x[p][i] = cut.keeps(i) ? xs[wave][cut.from - k0 + i] : 0.0f;
         }
@@ -179,8 +184,9 @@ template <typename X, typename W, int V, bool WHOLE> __global__ __launch_bounds_
     if (stores<16, 1>(lane)) a.t[(((size_t)blockIdx.y * a.N + n) * a.parts + part) * ranks + j0 + column_of<16, 1>(lane)] = sum[0] * alpha * col;
 }
 
-// t of up to TOKENS tokens from n0 on to LDS, rows of `pitch`: the parts added up in order.  THREADS / TOKENS threads share a token, each of them with four adjacent
-// ranks at a time, RANKS ranks in a turn.  Tokens without adapter get what happens to lie there.  Returns the largest finite |t| of this thread's.
+// t of up to TOKENS tokens from n0 on to LDS, rows of `pitch`: the parts added up in order.  THREADS / TOKENS threads share a token, each of them
+// with four adjacent ranks at a time, RANKS ranks in a turn.  Tokens without adapter get what happens to lie there.  Returns the largest finite |t|
+// of this thread's.
 template <int THREADS, int RANKS, int TOKENS = 64> struct GatherT {
     static constexpr int SHARE = THREADS / TOKENS, AT_ONCE = 4, OWN = RANKS / (SHARE * 4);
     static_assert(RANKS % (SHARE * 4) == 0 && OWN >= 1, "whole turns");
@@ -199,7 +205,8 @@ template <int THREADS, int RANKS, int TOKENS = 64> struct GatherT {
     }
     static __device__ __forceinline__ float finite(float v) { return fabsf(v) < INFINITY ? fabsf(v) : 0.0f; }
     // Sends for the first of it.
-    __device__ __forceinline__ GatherT(const ExpandArgs &a, int n0, int tokens) : parts(a.parts), ranks(ranks16(a.rank)), c((int)threadIdx.x / SHARE), share((int)threadIdx.x % SHARE), mine(c < tokens) {
+    __device__ __forceinline__ GatherT(const ExpandArgs &a, int n0, int tokens)
+        : parts(a.parts), ranks(ranks16(a.rank)), c((int)threadIdx.x / SHARE), share((int)threadIdx.x % SHARE), mine(c < tokens) {
         from = reinterpret_cast<const float4 *>(a.t + ((size_t)blockIdx.y * a.N + n0 + c) * parts * ranks);
         fetch(0, 0);
     }
@@ -228,12 +235,14 @@ template <int THREADS, int RANKS, int TOKENS = 64> struct GatherT {
 };
 
 // Y of V tokens of a row: the projection's result, scaled, and what the adapter adds.
-template <typename C, typename W, int V> __device__ __forceinline__ void finish(const float (&c)[V], const float (&col)[V], float row, const float (&add)[V], W (&y)[V]) {
+template <typename C, typename W, int V>
+__device__ __forceinline__ void finish(const float (&c)[V], const float (&col)[V], float row, const float (&add)[V], W (&y)[V]) {
 #pragma unroll
     for (int v = 0; v < V; ++v) y[v] = (W)((std::is_same<C, int32_t>::value ? c[v] * col[v] * row : c[v]) + add[v]);
 }
 
-// A workgroup does 64 rows of Y for 16 * EACH tokens: a wave takes EACH of them, its lane l row l; the sums meet the rows of C through LDS, so that both are read and written along the rows.
+// A workgroup does 64 rows of Y for 16 * EACH tokens: a wave takes EACH of them, its lane l row l; the sums meet the rows of C through LDS, so that
+// both are read and written along the rows.
 constexpr int kExpandRows = 64, kExpandThreads = 1024, kExpandWaves = kExpandThreads / 64;
 
 template <typename C, typename W, int EACH, bool WHOLE> __global__ __launch_bounds__(kExpandThreads) void expand_tokens_kernel(const ExpandArgs a) {
@@ -260,7 +269,8 @@ template <typename C, typename W, int EACH, bool WHOLE> __global__ __launch_boun
         row[o] = i / tokens;
         token[o] = i - row[o] * tokens;
         C one[1];
-        load<C, 1>(from, row[o] < kExpandRows && m0 + row[o] < a.M ? ((uint32_t)(m0 + row[o]) * (uint32_t)a.ldc + (uint32_t)(n0 + token[o])) * (uint32_t)sizeof(C) : kNowhere, 0, one);
+        load<C, 1>(from, row[o] < kExpandRows && m0 + row[o] < a.M
+                       ? ((uint32_t)(m0 + row[o]) * (uint32_t)a.ldc + (uint32_t)(n0 + token[o])) * (uint32_t)sizeof(C) : kNowhere, 0, one);
         had[o] = one[0];
     }
     float s[EACH];
@@ -311,7 +321,8 @@ template <typename C, typename W, int EACH, bool WHOLE> __global__ __launch_boun
         }
 }
 
-// ---- One token: one kernel.  Every workgroup works t out for itself, as that is a few reads of `down` from L2, and less than a second kernel has to wait.
+// ---- One token: one kernel.  Every workgroup works t out for itself, as that is a few reads of `down` from L2, and less than a second kernel has
+// to wait.
 
 constexpr int kOneRank = 64, kOneSize = 1 << 16;   // most ranks; most elements of `down`
 constexpr int kOneRows = 64, kOneThreads = 1024, kOneShare = kOneThreads / kOneRows;   // kOneShare: threads of a row of Y
@@ -329,7 +340,8 @@ struct OneArgs {
 // x goes to LDS; then a wave does a row of `down` at a time, and 16 threads a row of `up`.
 template <typename X, typename C, typename W, bool WHOLE> __global__ __launch_bounds__(kOneThreads) void one_token_kernel(const OneArgs a) {
     constexpr bool SCALED = std::is_same<C, int32_t>::value;
-    constexpr int LANE = 16 / (int)sizeof(W), WAVES = kOneThreads / 64, PIECE = 64 * LANE, AT_ONCE = 8;   // elements of a wave's load; loads on their way at a time
+    // elements of a wave's load; loads on their way at a time
+    constexpr int LANE = 16 / (int)sizeof(W), WAVES = kOneThreads / 64, PIECE = 64 * LANE, AT_ONCE = 8;
     extern __shared__ __align__(16) float xs[];   // K, rounded up
     __shared__ __align__(16) float ts[kOneRank];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -367,7 +379,10 @@ template <typename X, typename C, typename W, bool WHOLE> __global__ __launch_bo
                 W w[AT_ONCE][LANE];
 #pragma unroll
                 for (int q = 0; q < AT_ONCE; ++q)
-                    if (k0 + q * PIECE < a.K) at_piece(k0 + q * PIECE, [&](auto cut) { cut.load(down, j < a.rank ? (uint32_t)j * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, w[q]); });
+                    if (k0 + q * PIECE < a.K)
+                        at_piece(k0 + q * PIECE, [&](auto cut) {
+                            cut.load(down, j < a.rank ? (uint32_t)j * (uint32_t)a.K * (uint32_t)sizeof(W) : kNowhere, w[q]);
+                        });
                 if (j0 == 0 && k0 == 0) __syncthreads();   // x is in LDS
 #pragma unroll
                 for (int q = 0; q < AT_ONCE; ++q)
@@ -412,9 +427,9 @@ template <typename X, typename C, typename W, bool WHOLE> __global__ __launch_bo
 
 // ---- Many tokens: tiles of 64 on the matrix cores.
 //
-// A lane has four adjacent tokens, one of each of four 16-wide tiles, so that x, C and Y are read and written 4 tokens at a time.  An adapter's weights meet
-// all tokens of a tile, of which only those that are its own take the result: nothing of another token or adapter reaches them.  Tokens of
-// a request lie side by side, so that a tile meets one adapter or two; a tile of 64 requests takes 64 turns.
+// A lane has four adjacent tokens, one of each of four 16-wide tiles, so that x, C and Y are read and written 4 tokens at a time.  An adapter's
+// weights meet all tokens of a tile, of which only those that are its own take the result: nothing of another token or adapter reaches them. 
+// Tokens of a request lie side by side, so that a tile meets one adapter or two; a tile of 64 requests takes 64 turns.
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
@@ -451,7 +466,9 @@ template <typename W> struct Step;
 template <> struct Step<_Float16> {
     static constexpr int ROWS = 32, LANE = 8;
     typedef half8 frag;
-    static __device__ __forceinline__ float4v mma(const frag &w, const frag &x, const float4v &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(w, x, c, 0, 0, 0); }
+    static __device__ __forceinline__ float4v mma(const frag &w, const frag &x, const float4v &c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(w, x, c, 0, 0, 0);
+    }
 };
 template <> struct Step<float> {
     static constexpr int ROWS = 16, LANE = 4;
@@ -465,10 +482,11 @@ template <> struct Step<float> {
 
 constexpr int kShrinkWaves = 8;
 
-// 2048 tokens of int8, K = 4096, rank 64: 13.6 us, a turn 1.2 (two parts of eight turns; four parts lengthen the second kernel by more).
-// A workgroup does 64 tokens and a part of K, its eight waves a step each at a time (256 rows of half weights, 128 of binary32); what a turn needs from
-// memory is fetched while the one before it is computed.  When an adapter's last turn is done, the waves' sums meet in LDS.
-template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds__(kShrinkWaves * 64, 2) void shrink_tiles_kernel(const ShrinkArgs a) {
+// 2048 tokens of int8, K = 4096, rank 64: 13.6 us, a turn 1.2 (two parts of eight turns; four parts lengthen the second kernel by more). A
+// workgroup does 64 tokens and a part of K, its eight waves a step each at a time (256 rows of half weights, 128 of binary32); what a turn needs
+// from memory is fetched while the one before it is computed.  When an adapter's last turn is done, the waves' sums meet in LDS.
+template <typename X, typename W, int RB, bool WHOLE>
+__global__ __launch_bounds__(kShrinkWaves * 64, 2) void shrink_tiles_kernel(const ShrinkArgs a) {
     typedef Step<W> Q;
     typedef typename Q::frag frag;
     constexpr int TURN = kShrinkWaves * Q::ROWS;
@@ -492,7 +510,8 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
         x_at[e] = tokens.columns.any ? ((uint32_t)(lane_row + e) * (uint32_t)a.ldx + (uint32_t)tokens.columns.first) * (uint32_t)sizeof(X) : kNowhere;
     // (Every fetch is made, if of nothing: where one might be left out, the compiler has to wait for the whole of the one before it.)
     // !WHOLE: how many rows up the piece begins that the end of K cuts short.
-    const int turns = (a.K + TURN - 1) / TURN, end_at = (turns - 1) * TURN + lane_row, up = !WHOLE && end_at < a.K ? max(0, end_at + Q::LANE - a.K) : 0;
+    const int turns = (a.K + TURN - 1) / TURN, end_at = (turns - 1) * TURN + lane_row;
+    const int up = !WHOLE && end_at < a.K ? max(0, end_at + Q::LANE - a.K) : 0;
     auto fetch_x = [&](bool any, int turn, Loads &l) {
         if constexpr (!WHOLE) {   // (a first row of the turn, less those rows, may lie before it)
             const uint32_t to = ((uint32_t)turn * (uint32_t)TURN - (turn + 1 == turns ? (uint32_t)up : 0u)) * (uint32_t)a.ldx * (uint32_t)sizeof(X);
@@ -501,17 +520,20 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
             return;
         }
 #pragma unroll
-        for (int e = 0; e < Q::LANE; ++e) load<X, 4>(from, any ? x_at[e] : kNowhere, (uint32_t)turn * (uint32_t)TURN * (uint32_t)a.ldx * (uint32_t)sizeof(X), l.v[e]);
+        for (int e = 0; e < Q::LANE; ++e)
+            load<X, 4>(from, any ? x_at[e] : kNowhere, (uint32_t)turn * (uint32_t)TURN * (uint32_t)a.ldx * (uint32_t)sizeof(X), l.v[e]);
     };
     auto fetch_w = [&](int id, int turn, Loads &l) {
         const Matrix down(id >= 0 ? static_cast<const W *>(a.down) + (size_t)id * a.rank * a.K : nullptr, a.rank, a.K, a.K, sizeof(W));
         const int k = turn * TURN + lane_row;
         if constexpr (WHOLE) {
-            const uint32_t at = k < a.K ? ((uint32_t)i * (uint32_t)a.K + (uint32_t)lane_row) * (uint32_t)sizeof(W) : kNowhere;   // (ranks past the last lie outside, too)
+            // (ranks past the last lie outside, too)
+            const uint32_t at = k < a.K ? ((uint32_t)i * (uint32_t)a.K + (uint32_t)lane_row) * (uint32_t)sizeof(W) : kNowhere;
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
                 W v[Q::LANE];
-                load<W, Q::LANE>(down, at + (k < a.K ? (uint32_t)(b * 16) * (uint32_t)a.K * (uint32_t)sizeof(W) : 0), id >= 0 ? (uint32_t)turn * (uint32_t)TURN * (uint32_t)sizeof(W) : 0, v);
+                load<W, Q::LANE>(down, at + (k < a.K ? (uint32_t)(b * 16) * (uint32_t)a.K * (uint32_t)sizeof(W) : 0),
+                                 id >= 0 ? (uint32_t)turn * (uint32_t)TURN * (uint32_t)sizeof(W) : 0, v);
                 __builtin_memcpy(&l.w[b], v, 16);
             }
         } else {
@@ -519,7 +541,8 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
                 W v[Q::LANE];
-                load<W, Q::LANE>(down, cut.any && b * 16 + i < a.rank ? ((uint32_t)(b * 16 + i) * (uint32_t)a.K + (uint32_t)cut.from) * (uint32_t)sizeof(W) : kNowhere, 0, v);
+                load<W, Q::LANE>(down, cut.any && b * 16 + i < a.rank
+                                     ? ((uint32_t)(b * 16 + i) * (uint32_t)a.K + (uint32_t)cut.from) * (uint32_t)sizeof(W) : kNowhere, 0, v);
                 cut.mask(v);
                 __builtin_memcpy(&l.w[b], v, 16);
             }
@@ -542,7 +565,8 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
 #pragma unroll
         for (int c = 0; c < 4; ++c) ids[i * 4 + c] = tokens.id[c];
     // Thread t: two ranks of a token, the waves' sums in their order.
-    const int item = t >> 1, of_c = item >> 6, of_lane = item & 63, n = min(n0 + (of_lane & 15) * 4, a.N - 4) + of_c, of_j = (of_lane >> 4) * 4 + (t & 1) * 2;
+    const int item = t >> 1, of_c = item >> 6, of_lane = item & 63, n = min(n0 + (of_lane & 15) * 4, a.N - 4) + of_c;
+    const int of_j = (of_lane >> 4) * 4 + (t & 1) * 2;
     float *const to = a.t + (((size_t)blockIdx.y * a.N + n) * a.parts + part) * ranks + of_j;
     const float col = a.col ? a.col[(size_t)blockIdx.y * a.N + n] : 1.0f;
     float4v acc[RB][4];
@@ -597,8 +621,8 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
                 sum.x = sum.x * alpha * col;
                 sum.y = sum.y * alpha * col;
                 if constexpr (std::is_same<W, float>::value) {
-                    // Ranks behind the last one are zeros, not what zeros for weights make of an infinite x: the second kernel multiplies them.  (For half it
-                    // makes sums that are not finite again, of the ranks there are.)
+                    // Ranks behind the last one are zeros, not what zeros for weights make of an infinite x: the second kernel multiplies them. 
+                    // (For half it makes sums that are not finite again, of the ranks there are.)
                     if (b * 16 + of_j >= a.rank) sum.x = 0.0f;
                     if (b * 16 + of_j + 1 >= a.rank) sum.y = 0.0f;
                 }
@@ -614,17 +638,18 @@ template <typename X, typename W, int RB, bool WHOLE> __global__ __launch_bounds
     while (step(even, odd) && step(odd, even)) {}
 }
 
-// 2048 tokens, 4096 rows, rank 64, int32 to half, 50 MB: 15 us where every tile meets one adapter, 19 with two, 23 with runs of random lengths, whose longest tile ends last; of it about 6 us before
-// the first block, in which t is gathered and made into operands.
-// Waves of a workgroup: the more ranks, the more of them share what is made of t first.
+// 2048 tokens, 4096 rows, rank 64, int32 to half, 50 MB: 15 us where every tile meets one adapter, 19 with two, 23 with runs of random lengths,
+// whose longest tile ends last; of it about 6 us before the first block, in which t is gathered and made into operands. Waves of a workgroup: the
+// more ranks, the more of them share what is made of t first.
 template <int RB> constexpr int kExpandTileWaves = RB < 4 ? 4 : 8;
 
-// A workgroup does 64 tokens and `rows` rows of Y (a multiple of 64), its waves 16 of them at a time; what such a block needs from memory is fetched while the one before it
-// is computed.
-// half: t is split into two halves, t = hi + lo, which the instruction's 32 steps take side by side for 16 ranks, beside the same 16 weights
-// twice: 22 bits of t, at a sixteenth of what binary32 instructions cost.  Every token's t is scaled by a power of two first, its largest finite one
-// to 2^14 ... 2^15, so that neither half leaves its range: what lo loses below 2^-24 is 2^-39 of that largest.  (An infinite t stays one, and has no lo.)
-template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds__(kExpandTileWaves<RB> * 64, RB < 2 ? 3 : 2) void expand_tiles_kernel(const ExpandArgs a) {
+// A workgroup does 64 tokens and `rows` rows of Y (a multiple of 64), its waves 16 of them at a time; what such a block needs from memory is
+// fetched while the one before it is computed. half: t is split into two halves, t = hi + lo, which the instruction's 32 steps take side by side
+// for 16 ranks, beside the same 16 weights twice: 22 bits of t, at a sixteenth of what binary32 instructions cost.  Every token's t is scaled by a
+// power of two first, its largest finite one to 2^14 ... 2^15, so that neither half leaves its range: what lo loses below 2^-24 is 2^-39 of that
+// largest.  (An infinite t stays one, and has no lo.)
+template <typename C, typename W, int RB, bool WHOLE>
+__global__ __launch_bounds__(kExpandTileWaves<RB> * 64, RB < 2 ? 3 : 2) void expand_tiles_kernel(const ExpandArgs a) {
     constexpr bool SCALED = std::is_same<C, int32_t>::value, HALF = std::is_same<W, _Float16>::value;
     typedef Step<W> Q;
     typedef typename Q::frag frag;
@@ -657,7 +682,8 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
     auto fetch_c = [&](int m, Block &b) {
         const bool some = m < end;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) load<C, 4>(from, some ? c_at[q] : kNowhere, some ? (uint32_t)m * (uint32_t)a.ldc * (uint32_t)sizeof(C) : 0, b.had[q]);
+        for (int q = 0; q < 4; ++q)
+            load<C, 4>(from, some ? c_at[q] : kNowhere, some ? (uint32_t)m * (uint32_t)a.ldc * (uint32_t)sizeof(C) : 0, b.had[q]);
         if constexpr (SCALED) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -721,7 +747,8 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
             const float *const from = ts + row_of(of) * PITCH + j0;
             float4v v[Q::LANE / 4];
 #pragma unroll
-            for (int p = 0; p < Q::LANE / 4; ++p) v[p] = id >= 0 && b * 16 < ranks ? *reinterpret_cast<const float4v *>(from + p * 4) : float4v{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int p = 0; p < Q::LANE / 4; ++p)
+                v[p] = id >= 0 && b * 16 < ranks ? *reinterpret_cast<const float4v *>(from + p * 4) : float4v{0.0f, 0.0f, 0.0f, 0.0f};
             frag f;
 #pragma unroll
             for (int e = 0; e < Q::LANE; ++e) {
@@ -760,7 +787,8 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
             for (int r = 0; r < RB; ++r)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    // (In binary32 a product is worth a branch around it: 512 requests of a token each, 4096 rows, rank 16: 19 us for 25.  In half it is not.)
+                    // (In binary32 a product is worth a branch around it: 512 requests of a token each, 4096 rows, rank 16: 19 us for 25.  In half
+                    // it is not.)
                     if (!HALF && !decltype(alone)::value && !__any(tokens.id[c] == id)) continue;
                     acc[c] = Q::mma(w[r], x[r][c], acc[c]);
                 }
@@ -803,7 +831,9 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
             }
         }
         if constexpr (HALF) {
-            // Halves of t say nothing about infinities: an infinite weight times lo is undefined or of any sign.  Sums that are not finite are made again from t itself.
+            // Halves of t say nothing about infinities: an infinite weight times lo is undefined or of any sign.  Sums that are not finite are made
+            // again from t itself. (It costs 0.1 us of 11.1 for 1024 tokens of prompts, 1024 -> 4096, rank 16; looking for infinite weights before
+            // every product 0.3, and 0.8 of 37 at rank 64.)
             float most = 0.0f;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
@@ -816,7 +846,8 @@ template <typename C, typename W, int RB, bool WHOLE> __global__ __launch_bounds
                     for (int c = 0; c < 4; ++c)
                         if (!(fabsf(add[q][c]) < INFINITY)) {
                             int of = tokens.id[c], n = tokens.columns.first + c - n0, at = m + g * 4 + q;
-                            asm volatile("" : "+v"(of), "+v"(n), "+v"(at));   // (or the addresses of all sixteen are reckoned ahead and fill the registers)
+                            // (or the addresses of all sixteen are reckoned ahead and fill the registers)
+                            asm volatile("" : "+v"(of), "+v"(n), "+v"(at));
                             if (of < 0 || at >= a.M) continue;
                             const W *const up = static_cast<const W *>(a.up) + ((size_t)of * a.M + at) * a.rank;
                             const float *const from = ts + row_of(n) * PITCH;
@@ -859,33 +890,50 @@ struct Plan {   // the kernels of a call, and what they go by
     int shrink_threads, expand_threads, lds;
 };
 
-template <typename X, typename W, int RB> const void *shrink_tiles(bool whole) { return whole ? (const void *)shrink_tiles_kernel<X, W, RB, true> : (const void *)shrink_tiles_kernel<X, W, RB, false>; }
-template <typename C, typename W, int RB> const void *expand_tiles(bool whole) { return whole ? (const void *)expand_tiles_kernel<C, W, RB, true> : (const void *)expand_tiles_kernel<C, W, RB, false>; }
-template <typename C, typename W, int EACH> const void *expand_tokens(bool whole) { return whole ? (const void *)expand_tokens_kernel<C, W, EACH, true> : (const void *)expand_tokens_kernel<C, W, EACH, false>; }
-template <typename X, typename W, int V> const void *shrink_tokens(bool whole) { return whole ? (const void *)shrink_tokens_kernel<X, W, V, true> : (const void *)shrink_tokens_kernel<X, W, V, false>; }
-
-template <typename X, typename C, typename W> const void *one_token(bool whole) { return whole ? (const void *)one_token_kernel<X, C, W, true> : (const void *)one_token_kernel<X, C, W, false>; }
+template <typename X, typename W, int RB> const void *shrink_tiles(bool whole) {
+    return whole ? (const void *)shrink_tiles_kernel<X, W, RB, true> : (const void *)shrink_tiles_kernel<X, W, RB, false>;
+}
+template <typename C, typename W, int RB> const void *expand_tiles(bool whole) {
+    return whole ? (const void *)expand_tiles_kernel<C, W, RB, true> : (const void *)expand_tiles_kernel<C, W, RB, false>;
+}
+template <typename C, typename W, int EACH> const void *expand_tokens(bool whole) {
+    return whole ? (const void *)expand_tokens_kernel<C, W, EACH, true> : (const void *)expand_tokens_kernel<C, W, EACH, false>;
+}
+template <typename X, typename W, int V> const void *shrink_tokens(bool whole) {
+    return whole ? (const void *)shrink_tokens_kernel<X, W, V, true> : (const void *)shrink_tokens_kernel<X, W, V, false>;
+}
+template <typename X, typename C, typename W> const void *one_token(bool whole) {
+    return whole ? (const void *)one_token_kernel<X, C, W, true> : (const void *)one_token_kernel<X, C, W, false>;
+}
 
 template <typename X, typename C, typename W> Plan plan_of(const sparsert_adapter_set &d) {
     Plan p{};
     constexpr int LANE = 16 / (int)sizeof(W);
     const bool whole_k = d.K % LANE == 0, whole_rank = d.rank % LANE == 0;
     const int ranks = (d.rank + 15) / 16 * 16;
-    // One token.  Measured as one kernel and as two, in us: K = 1024, ranks 8, 32, 64: half 3.6, 4.2, 5.7 and 5.6, 5.8, 6.3, binary32 3.6, 4.5, 6.0 and 5.7, 6.0, 6.6; K = 4096,
-    // rank 16: 4.7 and 6.0, 5.6 and 6.1, rank 32: 6.4 and 6.1, 7.9 and 6.4.  Odd K = 771, ranks 8, 32, 64: half 4.5, 6.0, 8.9 and 6.0, 6.2, 6.7, binary32 4.9, 7.1, 11.5 and 6.4, 6.7, 7.3.
+    // One token.  Measured as one kernel and as two, in us: K = 1024, ranks 8, 32, 64: half 3.6, 4.2, 5.7 and 5.6, 5.8, 6.3, binary32 3.6, 4.5, 6.0
+    // and 5.7, 6.0, 6.6; K = 4096, rank 16: 4.7 and 6.0, 5.6 and 6.1, rank 32: 6.4 and 6.1, 7.9 and 6.4.  Odd K = 771, ranks 8, 32, 64: half 4.5,
+    // 6.0, 8.9 and 6.0, 6.2, 6.7, binary32 4.9, 7.1, 11.5 and 6.4, 6.7, 7.3.
     if (d.N == 1 && d.rank <= kOneRank && (int64_t)ranks * d.K <= (whole_k ? kOneSize : kOneSize / 4)) {
         p.one = one_token<X, C, W>(whole_k);
         p.expand_grid = (d.M + kOneRows - 1) / kOneRows;
         p.lds = (d.K + 7) / 8 * 8 * (int)sizeof(float);
         return p;
     }
-    // Bytes of weights that the tokens read if every one reads its own: what the first kind of kernels spends its time on.  The other kind spends it on the adapters that
-    // a tile meets, which only the device knows, so the limit grows with their number.  4096 x 4096, rank 16, half, 24 adapters, tokens and tiles, us: 64 tokens in
-    // runs 8.2 and 9.2, 256 13.3 and 9.8, 512 21 and 11; 64 requests of a token each 9.5 and 18, 512 23 and 29.  Over 405 calls the choices come to 3 % above the best of each.
+    // Bytes of weights that the tokens read if every one reads its own: what the first kind of kernels spends its time on.  The other kind spends
+    // it on the adapters that a tile meets, which only the device knows, so the limit grows with their number.  4096 x 4096, rank 16, half, 24
+    // adapters, tokens and tiles, us: 64 tokens in runs 8.2 and 9.2, 256 13.3 and 9.8, 512 21 and 11; 64 requests of a token each 9.5 and 18, 512
+    // 23 and 29.  Over 405 calls of 8 to 512 tokens, with 2 and 24 adapters, the choices come to 3 % above the best of each.  What they miss is a
+    // batch that meets few of many adapters, or many of few: 1024 -> 4096, 1024 tokens, rank 16 in half, tokens and tiles: in runs with 32 adapters
+    // 25.9 and 11.5 (tiles), with 64 25.6 and 11.9 (tokens); requests of a token each with 24 26.1 and 32.5 (tiles), with 64 27.0 and 49.7
+    // (tokens); 4096 x 4096, 2048 requests, 64 adapters 73 and 128 (tiles). Tiles are built for ranks up to 64, and for rows of weights that are
+    // read in pieces (pieces_fit).  Beyond them tokens take what is left: 4096 x 4096, 2048 tokens, half, rank 64 37 us in tiles, 65 601, 96 245,
+    // 128 404, 256 716; 1024 -> 4096, rank 8 14.8, 6 17.0, 7 102.
     const double own = (double)d.N * d.batch * ((double)d.M + d.K) * ranks * (int)sizeof(W);
     const double limit = (30e6 + 4e6 * std::min(d.count, kTile)) * (sizeof(W) == 4 ? 2 : 1);
     // (The tiles' lanes reckon with offsets of some rows on from any one.)
-    const bool near = (int64_t)(kShrinkWaves * Step<W>::ROWS) * d.ldx * (int)sizeof(X) < 1ll << 31 && 16ll * std::max((int64_t)d.ldc * (int)sizeof(C), (int64_t)d.ldy * (int)sizeof(W)) < 1ll << 31 &&
+    const bool near = (int64_t)(kShrinkWaves * Step<W>::ROWS) * d.ldx * (int)sizeof(X) < 1ll << 31 &&
+        16ll * std::max((int64_t)d.ldc * (int)sizeof(C), (int64_t)d.ldy * (int)sizeof(W)) < 1ll << 31 &&
                       64ll * d.K * (int)sizeof(W) < 1ll << 31 && 16ll * d.rank * (int)sizeof(W) < 1ll << 31;
     if (near && d.N >= 4 && d.rank <= 64 && pieces_fit<W>(d.rank) && d.K >= LANE && own > limit) {
         const int64_t tiles = ((int64_t)d.N + kTile - 1) / kTile;
@@ -897,7 +945,8 @@ template <typename X, typename C, typename W> Plan plan_of(const sparsert_adapte
         p.slots = (int)std::min<int64_t>({8, d.count, std::max<int64_t>(1, 256 / (tiles * d.batch * p.parts))});
         p.shrink = ranks <= 16 ? shrink_tiles<X, W, 1>(whole_k) : ranks <= 32 ? shrink_tiles<X, W, 2>(whole_k) : shrink_tiles<X, W, 4>(whole_k);
         p.shrink_grid = tiles * p.parts * p.slots; p.shrink_threads = kShrinkWaves * 64;
-        p.expand = ranks <= 16 ? expand_tiles<C, W, 1>(whole_rank) : ranks <= 32 ? expand_tiles<C, W, 2>(whole_rank) : expand_tiles<C, W, 4>(whole_rank);
+        p.expand = ranks <= 16 ? expand_tiles<C, W, 1>(whole_rank)
+                 : ranks <= 32 ? expand_tiles<C, W, 2>(whole_rank) : expand_tiles<C, W, 4>(whole_rank);
         const int step = ranks <= 32 ? kExpandTileWaves<2> * 16 : kExpandTileWaves<4> * 16;
         const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>((d.M + step - 1) / step, (ranks <= 32 ? 512 : 256) / (tiles * d.batch)));
         p.rows = (int)(((d.M + chunks - 1) / chunks + step - 1) / step * step);
@@ -909,7 +958,9 @@ template <typename X, typename C, typename W> Plan plan_of(const sparsert_adapte
     p.shrink_grid = ((int64_t)d.N + kTokenGroup - 1) / kTokenGroup * p.parts * (ranks / 16); p.shrink_threads = kTokenThreads;
     const int64_t blocks = (d.M + kExpandRows - 1) / kExpandRows;
     int each = 4;
-    while (each > 1 && (blocks * (((int64_t)d.N + each * kExpandWaves - 1) / (each * kExpandWaves)) * d.batch < 256 || each * kExpandWaves * ranks > 8192)) each /= 2;   // (t of 32 KiB at most in LDS)
+    // (t of 32 KiB at most in LDS)
+    while (each > 1 && (blocks * (((int64_t)d.N + each * kExpandWaves - 1) / (each * kExpandWaves)) * d.batch < 256 ||
+        each * kExpandWaves * ranks > 8192)) each /= 2;
     p.expand = each == 4 ? expand_tokens<C, W, 4>(whole_rank) : each == 2 ? expand_tokens<C, W, 2>(whole_rank) : expand_tokens<C, W, 1>(whole_rank);
     p.expand_grid = ((int64_t)d.N + each * kExpandWaves - 1) / (each * kExpandWaves) * blocks; p.expand_threads = kExpandThreads;
     p.lds = each * kExpandWaves * ranks * (int)sizeof(float);
@@ -924,7 +975,9 @@ Plan plan_of(const sparsert_adapter_set &d) {
 
 }  // namespace
 
-size_t adapters_workspace(const sparsert_adapter_set &d) { return (size_t)d.batch * d.N * plan_of(d).parts * ((d.rank + 15) / 16 * 16) * sizeof(float); }
+size_t adapters_workspace(const sparsert_adapter_set &d) {
+    return (size_t)d.batch * d.N * plan_of(d).parts * ((d.rank + 15) / 16 * 16) * sizeof(float);
+}
 
 int launch_adapters(const AdaptersCall &c, std::string &err) {
     const sparsert_adapter_set &d = c.d;

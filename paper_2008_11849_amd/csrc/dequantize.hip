@@ -1,7 +1,8 @@
 // The int32 result of an int8 product times its row and column scales: y = c col row, in binary32, rounded once.
 //
-// Bound by memory: every element is read and written once.  4096 rows of 4093 in 4097, to binary32, 134 MB: 28.5 us, 4.7 TB/s, nine tenths of a large copy's rate (rows of odd pitch
-// begin anywhere: vectors are read and written wherever they lie).  768 x 1024 to half: 2.5 us, of which 1.7 are a kernel that does nothing.
+// Bound by memory: every element is read and written once.  4096 rows of 4093 in 4097, to binary32, 134 MB: 28.4 us, 4.7 TB/s, nine tenths of a
+// large copy's rate (rows of odd pitch begin anywhere: vectors are read and written wherever they lie).  768 x 1024 to half: 2.5 us, of which 1.7
+// are a kernel that does nothing.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -19,9 +20,9 @@ struct DequantArgs {
     int32_t M, N, ldc, ldy;
 };
 
-// Strips as wide as the row allows, so that a wave reads a kilobyte of it at once.
-// A workgroup of 256 threads does a strip of V * L columns in kDequantPasses * 256 / L rows: thread t has the V columns of lane t % L in the rows t / L, t / L +
-// 256 / L, ...  All of its rows are fetched before the first is scaled.
+// Strips as wide as the row allows, so that a wave reads a kilobyte of it at once. A workgroup of 256 threads does a strip of V * L columns in
+// kDequantPasses * 256 / L rows: thread t has the V columns of lane t % L in the rows t / L, t / L + 256 / L, ...  All of its rows are fetched
+// before the first is scaled.
 constexpr int kDequantThreads = 256, kDequantPasses = 4;
 
 template <typename T, int V, int L> __global__ __launch_bounds__(kDequantThreads) void dequantize_kernel(const DequantArgs a) {
@@ -32,7 +33,8 @@ template <typename T, int V, int L> __global__ __launch_bounds__(kDequantThreads
     const int strip = task % strips, first = task / strips * BLOCK;
     const int row = (int)threadIdx.x / L;
     const Columns<V> columns(strip * W + (int)threadIdx.x % L * V, a.N);
-    const Matrix C(a.C + (int64_t)blockIdx.y * a.M * a.ldc, a.M, a.N, a.ldc, 4), Y(static_cast<T *>(a.Y) + (int64_t)blockIdx.y * a.M * a.ldy, a.M, a.N, a.ldy, sizeof(T));
+    const Matrix C(a.C + (int64_t)blockIdx.y * a.M * a.ldc, a.M, a.N, a.ldc, 4);
+    const Matrix Y(static_cast<T *>(a.Y) + (int64_t)blockIdx.y * a.M * a.ldy, a.M, a.N, a.ldy, sizeof(T));
     const Matrix R(a.row, 1, a.M, a.M, 4), S(a.col ? a.col + (int64_t)blockIdx.y * a.N : nullptr, 1, a.N, a.N, 4);
     float col[V];
 #pragma unroll
@@ -84,7 +86,8 @@ int launch_dequantize(const DequantCall &c, std::string &err) {
     const int64_t strips = (vectors + lanes - 1) / lanes, rows = kDequantThreads / lanes * kDequantPasses;
     const int64_t blocks = (d.M + rows - 1) / rows, tasks = strips * blocks;
     const bool half = d.dtype == SPARSERT_F16;
-    const void *kernel = V == 1 ? half ? dequantize_of<_Float16, 1>(lanes) : dequantize_of<float, 1>(lanes) : half ? dequantize_of<_Float16, 4>(lanes) : dequantize_of<float, 4>(lanes);
+    const void *kernel = V == 1 ? half ? dequantize_of<_Float16, 1>(lanes) : dequantize_of<float, 1>(lanes)
+                                : half ? dequantize_of<_Float16, 4>(lanes) : dequantize_of<float, 4>(lanes);
     return launch_operator(kernel, dim3((uint32_t)((tasks + 7) / 8 * 8), (uint32_t)d.batch), kDequantThreads, a, c.stream, err);
 }
 

@@ -1,11 +1,13 @@
 // Root-mean-square norm over the features of every token, with the residual's addition and, for int8 products, quantisation.
 //
-// h = x + r,  v = h gamma,  f = 1 / sqrt(sum h^2 / K + eps),  y = v f.  int8: y = round(127 v / a) with a = max |v|, scale a f / 127: f drops out of
-// the integers, so that the sum of squares and the maximum come from one pass.  A token is a column: its sums run down the rows, lanes of a wave lie along them, so
-// that rows are read in runs, and columns meet in LDS.  Everything is held in binary32 and rounded once, at the stores; sums are added in one order, whatever the timing.
+// h = x + r,  v = h gamma,  f = 1 / sqrt(sum h^2 / K + eps),  y = v f.  int8: y = round(127 v / a) with a = max |v|, scale a f / 127: f drops out
+// of the integers, so that the sum of squares and the maximum come from one pass.  A token is a column: its sums run down the rows, lanes of a wave
+// lie along them, so that rows are read in runs, and columns meet in LDS.  Everything is held in binary32 and rounded once, at the stores; sums are
+// added in one order, whatever the timing.
 //
-// Bounds: the wait for one read of memory and for two rounds through LDS in small calls (K = 1024, one token: 2.3 us, of which 1.7 are a kernel that does
-// nothing), memory in large ones: 4096 x 4096 half with both residuals, 134 MB: 33.6 us, 4.0 TB/s, where two copies of as many bytes take 28.2 us.
+// Bounds: the wait for one read of memory and for two rounds through LDS in small calls (K = 1024, one token: 2.3 us, of which 1.7 are a kernel
+// that does nothing), memory in large ones: 4096 x 4096 half with both residuals, 134 MB: 33.6 us, 4.0 TB/s, where two copies of as many bytes take
+// 28.2 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -29,7 +31,8 @@ struct NormArgs {
     int32_t parts, rows;   // parts of a column, and rows of each
 };
 
-// 1 / sqrt(m), rounded once: a root and a quotient are two roundings, 1.5 times as far off.  A step of Newton's from there, on what is left of m r r to 1, exactly.
+// 1 / sqrt(m), rounded once: a root and a quotient are two roundings, 1.5 times as far off.  A step of Newton's from there, on what is left of m r^2
+// to 1, exactly.
 __device__ __forceinline__ float reciprocal_root(float m) {
     const float r = 1.0f / sqrtf(m), h = m * r, rest = __builtin_fmaf(-h, r, 1.0f) - __builtin_fmaf(m, r, -h) * r;
     return r > 0.0f ? __builtin_fmaf(0.5f * r, rest, r) : r;   // (of infinity it is 0)
@@ -59,7 +62,8 @@ template <typename T, int V, int L, int THREADS> struct Rows {
     __device__ __forceinline__ Rows(const NormArgs &a, int strip, int first, int end)
         : a(a), row((int)threadIdx.x / L), first(first), end(end), columns(strip * W + (int)threadIdx.x % L * V, a.N),
           X(static_cast<const T *>(a.X) + (int64_t)blockIdx.y * a.K * a.ldx, a.K, a.N, a.ldx, sizeof(T)),
-          R(a.R ? static_cast<const T *>(a.R) + (int64_t)blockIdx.y * a.K * a.ldh : nullptr, a.K, a.N, a.ldh, sizeof(T)), G(a.gamma, 1, a.K, a.K, sizeof(float)) {}
+          R(a.R ? static_cast<const T *>(a.R) + (int64_t)blockIdx.y * a.K * a.ldh : nullptr, a.K, a.N, a.ldh, sizeof(T)),
+          G(a.gamma, 1, a.K, a.K, sizeof(float)) {}
     // This thread's byte in pass i of the rows from k0 on.
     __device__ __forceinline__ uint32_t place(int k0, int i, int ld, int size, uint32_t &common) const {
         const int at = k0 + i * ROWS;
@@ -90,14 +94,16 @@ template <typename T, int V, int L, int THREADS> struct Rows {
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
             const int k = k0 + i * ROWS + row;
-            g[i] = a.gamma ? __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(G.at, k < end ? (uint32_t)k * 4u : kNowhere, 0, 0)) : 1.0f;
+            g[i] = a.gamma ? __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(G.at, k < end ? (uint32_t)k * 4u : kNowhere, 0, 0))
+                : 1.0f;
         }
 #pragma unroll
         for (int i = 0; i < PASSES; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) h[i][v] = (float)x[i][v] + (float)r[i][v];
     }
-    template <typename Out, int PASSES, int AUX = 0, typename F> __device__ __forceinline__ void write(const Matrix &m, int k0, int ld, F value) const {
+    template <typename Out, int PASSES, int AUX = 0, typename F>
+    __device__ __forceinline__ void write(const Matrix &m, int k0, int ld, F value) const {
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
             Out out[V];
@@ -111,11 +117,15 @@ template <typename T, int V, int L, int THREADS> struct Rows {
 };
 
 template <typename T, bool QUANT> using out_t = typename std::conditional<QUANT, int8_t, T>::type;
-template <typename T> __device__ __forceinline__ Matrix sum_of(const NormArgs &a) { return Matrix(a.H ? static_cast<T *>(a.H) + (int64_t)blockIdx.y * a.K * a.ldh : nullptr, a.K, a.N, a.ldh, sizeof(T)); }
-template <typename Out> __device__ __forceinline__ Matrix result_of(const NormArgs &a) { return Matrix(static_cast<Out *>(a.Y) + (int64_t)blockIdx.y * a.K * a.ldy, a.K, a.N, a.ldy, sizeof(Out)); }
+template <typename T> __device__ __forceinline__ Matrix sum_of(const NormArgs &a) {
+    return Matrix(a.H ? static_cast<T *>(a.H) + (int64_t)blockIdx.y * a.K * a.ldh : nullptr, a.K, a.N, a.ldh, sizeof(T));
+}
+template <typename Out> __device__ __forceinline__ Matrix result_of(const NormArgs &a) {
+    return Matrix(static_cast<Out *>(a.Y) + (int64_t)blockIdx.y * a.K * a.ldy, a.K, a.N, a.ldy, sizeof(Out));
+}
 
 // ---- One kernel: a workgroup of THREADS threads does a strip.  HELD: PASSES passes are all rows, and stay in registers between the
-// sums and the results; otherwise the rows are fetched twice.  768 x 1024 half to int8: 5.0 us; 4096 x 16: 5.8 us.
+// sums and the results; otherwise the rows are fetched twice.  768 x 1024 half to int8: 5.0 us; 4096 x 16: 5.7 us.
 template <typename T, bool QUANT, int V, int L, int PASSES, bool HELD, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs a) {
     typedef out_t<T, QUANT> Out;
@@ -185,9 +195,10 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs a) {
     }
 }
 
-// ---- Two kernels, for columns too few and too long to fill the GPU, and for calls beyond the caches: sums of every part of a strip, then the results.  A part is
-// `rows` rows of a strip.  The second kernel reads the rows again, from the caches (of 4096 x 4096 half, 67 MB, from the one beside
-// memory).  1027 x 771 of 784, binary32: 7.2 us.  The parts' sums and largest values lie in the caller's workspace, [batch][part][1 or 2][N].
+// ---- Two kernels, for columns too few and too long to fill the GPU, and for calls beyond the caches: sums of every part of a strip, then the
+// results.  A part is `rows` rows of a strip.  The second kernel reads the rows again, from the caches (of 4096 x 4096 half, 67 MB, from the one
+// beside memory).  1027 x 771 of 784, binary32: 7.1 us.  The parts' sums and largest values lie in the caller's workspace, [batch][part][1 or
+// 2][N].
 constexpr int kPartThreads = 256, kWideLanes = 16;
 constexpr int kPartPasses = 4;    // rows of a thread that are fetched at a time
 constexpr int kPartsAtOnce = 8;   // sums that a thread of the second kernel fetches at a time
@@ -308,8 +319,10 @@ template <typename T, bool QUANT, int V, int L> const void *norm_of(int K) {
     return (const void *)norm_kernel<T, QUANT, V, L, 4, false, kNormThreads>;
 }
 
-// Columns of a lane and lanes of a strip: 16 bytes, and as many lanes as leave 256 workgroups; narrower than that, one column to a lane.  Where a lane is a strip and 128 columns or
-// fewer are all, four columns in half, too: 4096 x 16 to int8 5.8 us, with eight 6.6; but 768 x 1024 5.6 and 5.0.
+// Columns of a lane and lanes of a strip: 16 bytes, and as many lanes as leave 256 workgroups; narrower than that, one column to a lane.  Where a
+// lane is a strip and 128 columns or fewer are all, four columns in half, too.  Four and eight, in us, to int8: 4096 x 8 5.1 and 6.2, x 16 5.8 and
+// 6.5, x 32 8.4 and 8.3; 1024 x 8 3.3 and 3.6, x 128 4.7 and 4.7, x 384 5.3 and 5.1, x 1024 6.5 and 5.7.  From 32 to 256 columns they are within 5
+// % of each other in calls that are one kernel.
 template <typename T> void strip_shape(const sparsert_norm &d, int &V, int &L) {
     V = 16 / sizeof(T);
     if (d.N < V) {
@@ -331,11 +344,12 @@ template <typename T, bool QUANT> const void *norm_of(const sparsert_norm &d, in
         if (V == 1 && L == 8) return norm_of<T, QUANT, 1, 8>(d.K);
     if (V == 1) return L == 4 ? norm_of<T, QUANT, 1, 4>(d.K) : L == 2 ? norm_of<T, QUANT, 1, 2>(d.K) : norm_of<T, QUANT, 1, 1>(d.K);
     if (V == 4 && L == 1) return norm_of<T, QUANT, 4, 1>(d.K);
-    return L == 8 ? norm_of<T, QUANT, W, 8>(d.K) : L == 4 ? norm_of<T, QUANT, W, 4>(d.K) : L == 2 ? norm_of<T, QUANT, W, 2>(d.K) : norm_of<T, QUANT, W, 1>(d.K);
+    return L == 8 ? norm_of<T, QUANT, W, 8>(d.K) : L == 4 ? norm_of<T, QUANT, W, 4>(d.K)
+         : L == 2 ? norm_of<T, QUANT, W, 2>(d.K) : norm_of<T, QUANT, W, 1>(d.K);
 }
 
-// Estimate of a call as one kernel, fitted to calls of one to 4096 tokens of 768 to 8192 rows: a turn of the loads costs its wait and what the strip's narrowness wastes of
-// the lines that it touches.
+// Estimate of a call as one kernel, fitted (with eight halves to a lane) to calls of one to 4096 tokens of 768 to 8192 rows: a turn of the loads
+// costs its wait and what the strip's narrowness wastes of the lines that it touches.
 template <typename T> double one_kernel_us(const sparsert_norm &d, double bytes) {
     int V, L;
     strip_shape<T>(d, V, L);
@@ -354,22 +368,26 @@ template <typename T, bool QUANT, int V, int L, bool FAR = false> SplitNorm spli
     const int64_t most = std::min<int64_t>((d.K + ROWS - 1) / ROWS, kPartThreads / W * kPartsAtOnce);
     const int64_t parts = std::min(most, std::max<int64_t>(1, workgroups / ((int64_t)strips * d.batch)));
     const int rows = (int)((d.K + parts - 1) / parts);
-    return {(d.K + rows - 1) / rows, rows, strips, (const void *)norm_sums_kernel<T, QUANT, V, L>, (const void *)norm_results_kernel<T, QUANT, V, L, FAR>};
+    return {(d.K + rows - 1) / rows, rows, strips, (const void *)norm_sums_kernel<T, QUANT, V, L>,
+            (const void *)norm_results_kernel<T, QUANT, V, L, FAR>};
 }
 
 template <typename T, bool QUANT> SplitNorm split_of(const sparsert_norm &d) {
     constexpr int V = 16 / sizeof(T);
     const double bytes = (double)d.K * d.N * d.batch * (3 * sizeof(T) + sizeof(out_t<T, QUANT>));
-    // One kernel and two, measured in us (half): 1024 x 16 3.4 and 6.1, 768 x 1024 5.1 and 6.2, 2048 x 1024 10.3 and 7.7, 4096 x 128 12.9 and 6.5, 8192 x 1024
-    // 37 and 20.  Over 180 sizes the choices come to 0.6 % above the best of each.
+    // One kernel and two, measured in us (half): 1024 x 16 3.4 and 6.1, 768 x 1024 5.1 and 6.2, 2048 x 1024 10.3 and 7.7, 4096 x 128 12.9 and 6.5,
+    // 8192 x 1024 37 and 20.  Over 232 sizes, of half and binary32 to themselves and to int8, the choices come to 0.4 % above the best of each,
+    // with 13 % at most (4096 x 16 half 6.2 and 5.5).
     if (one_kernel_us<T>(d, bytes) <= (QUANT ? 6.2 : 5.3) + bytes / 4.4e6) return {};
     if constexpr (V > 4)
         if (d.N > 4 && d.N < V) return split_with<T, QUANT, 1, 8>(d, 256);
     if (d.N < V) return d.N > 2 ? split_with<T, QUANT, 1, 4>(d, 256) : split_with<T, QUANT, 1, 2>(d, 256);
-    // Strips of 8 vectors and of 16 (wide): 4096 x 1024 half 12.0 and 14.9, binary32 (67 MB) 19.2 and 18.1, 8192 x 1024 binary32 41 and 33, 4096 x 4096 half 44 and 34.
-    // H kept in the caches and not: 4096 x 4096 half 41.0 and 33.6, with a reader of Y and a later one of H behind it 72.5 and 69.2; 2048 x 4096 (67 MB) with the readers 37.0 and 38.4.
+    // Strips of 8 vectors and of 16 (wide): 4096 x 1024 half 12.0 and 14.9, binary32 (67 MB) 19.2 and 18.1, 8192 x 1024 binary32 41 and 33, 4096 x
+    // 4096 half 44 and 34. H kept in the caches and not: 4096 x 4096 half 41.0 and 33.6, with a reader of Y and a later one of H behind it 72.5 and
+    // 69.2; 2048 x 4096 (67 MB) with the readers 37.0 and 38.4.
     constexpr int64_t wide = V * kWideLanes;
-    if (bytes > 40e6 && d.batch * (d.N / wide) * (kPartThreads / wide * kPartsAtOnce) >= 256) return bytes > 100e6 ? split_with<T, QUANT, V, kWideLanes, true>(d, 512) : split_with<T, QUANT, V, kWideLanes>(d, 512);
+    if (bytes > 40e6 && d.batch * (d.N / wide) * (kPartThreads / wide * kPartsAtOnce) >= 256)
+        return bytes > 100e6 ? split_with<T, QUANT, V, kWideLanes, true>(d, 512) : split_with<T, QUANT, V, kWideLanes>(d, 512);
     return d.N > 4 * V ? split_with<T, QUANT, V, 8>(d, 256) : d.N > 2 * V ? split_with<T, QUANT, V, 4>(d, 256)
          : d.N > V ? split_with<T, QUANT, V, 2>(d, 256) : split_with<T, QUANT, V, 1>(d, 256);
 }
