@@ -340,7 +340,7 @@ struct OneArgs {
 // x goes to LDS; then a wave does a row of `down` at a time, and 16 threads a row of `up`.
 template <typename X, typename C, typename W, bool WHOLE> __global__ __launch_bounds__(kOneThreads) void one_token_kernel(const OneArgs a) {
     constexpr bool SCALED = std::is_same<C, int32_t>::value;
-    // elements of a wave's load; loads on their way at a time
+    // PIECE: elements of a wave's load; AT_ONCE: loads on their way at a time
     constexpr int LANE = 16 / (int)sizeof(W), WAVES = kOneThreads / 64, PIECE = 64 * LANE, AT_ONCE = 8;
     extern __shared__ __align__(16) float xs[];   // K, rounded up
     __shared__ __align__(16) float ts[kOneRank];
@@ -428,7 +428,7 @@ template <typename X, typename C, typename W, bool WHOLE> __global__ __launch_bo
 // ---- Many tokens: tiles of 64 on the matrix cores.
 //
 // A lane has four adjacent tokens, one of each of four 16-wide tiles, so that x, C and Y are read and written 4 tokens at a time.  An adapter's
-// weights meet all tokens of a tile, of which only those that are its own take the result: nothing of another token or adapter reaches them. 
+// weights meet all tokens of a tile, of which only those that are its own take the result: nothing of another token or adapter reaches them.
 // Tokens of a request lie side by side, so that a tile meets one adapter or two; a tile of 64 requests takes 64 turns.
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -482,8 +482,8 @@ template <> struct Step<float> {
 
 constexpr int kShrinkWaves = 8;
 
-// 2048 tokens of int8, K = 4096, rank 64: 13.6 us, a turn 1.2 (two parts of eight turns; four parts lengthen the second kernel by more). A
-// workgroup does 64 tokens and a part of K, its eight waves a step each at a time (256 rows of half weights, 128 of binary32); what a turn needs
+// 2048 tokens of int8, K = 4096, rank 64: 13.6 us, a turn 1.2 (two parts of eight turns; four parts lengthen the second kernel by more).
+// A workgroup does 64 tokens and a part of K, its eight waves a step each at a time (256 rows of half weights, 128 of binary32); what a turn needs
 // from memory is fetched while the one before it is computed.  When an adapter's last turn is done, the waves' sums meet in LDS.
 template <typename X, typename W, int RB, bool WHOLE>
 __global__ __launch_bounds__(kShrinkWaves * 64, 2) void shrink_tiles_kernel(const ShrinkArgs a) {
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(kShrinkWaves * 64, 2) void shrink_tiles_kernel(cons
         const Matrix down(id >= 0 ? static_cast<const W *>(a.down) + (size_t)id * a.rank * a.K : nullptr, a.rank, a.K, a.K, sizeof(W));
         const int k = turn * TURN + lane_row;
         if constexpr (WHOLE) {
-            // (ranks past the last lie outside, too)
+            // (Ranks past the last lie outside, too.)
             const uint32_t at = k < a.K ? ((uint32_t)i * (uint32_t)a.K + (uint32_t)lane_row) * (uint32_t)sizeof(W) : kNowhere;
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
@@ -621,7 +621,7 @@ __global__ __launch_bounds__(kShrinkWaves * 64, 2) void shrink_tiles_kernel(cons
                 sum.x = sum.x * alpha * col;
                 sum.y = sum.y * alpha * col;
                 if constexpr (std::is_same<W, float>::value) {
-                    // Ranks behind the last one are zeros, not what zeros for weights make of an infinite x: the second kernel multiplies them. 
+                    // Ranks behind the last one are zeros, not what zeros for weights make of an infinite x: the second kernel multiplies them.
                     // (For half it makes sums that are not finite again, of the ranks there are.)
                     if (b * 16 + of_j >= a.rank) sum.x = 0.0f;
                     if (b * 16 + of_j + 1 >= a.rank) sum.y = 0.0f;
@@ -639,12 +639,13 @@ __global__ __launch_bounds__(kShrinkWaves * 64, 2) void shrink_tiles_kernel(cons
 }
 
 // 2048 tokens, 4096 rows, rank 64, int32 to half, 50 MB: 15 us where every tile meets one adapter, 19 with two, 23 with runs of random lengths,
-// whose longest tile ends last; of it about 6 us before the first block, in which t is gathered and made into operands. Waves of a workgroup: the
-// more ranks, the more of them share what is made of t first.
+// whose longest tile ends last; of it about 6 us before the first block, in which t is gathered and made into operands.
+// Waves of a workgroup: the more ranks, the more of them share what is made of t first.
 template <int RB> constexpr int kExpandTileWaves = RB < 4 ? 4 : 8;
 
 // A workgroup does 64 tokens and `rows` rows of Y (a multiple of 64), its waves 16 of them at a time; what such a block needs from memory is
-// fetched while the one before it is computed. half: t is split into two halves, t = hi + lo, which the instruction's 32 steps take side by side
+// fetched while the one before it is computed.
+// half: t is split into two halves, t = hi + lo, which the instruction's 32 steps take side by side
 // for 16 ranks, beside the same 16 weights twice: 22 bits of t, at a sixteenth of what binary32 instructions cost.  Every token's t is scaled by a
 // power of two first, its largest finite one to 2^14 ... 2^15, so that neither half leaves its range: what lo loses below 2^-24 is 2^-39 of that
 // largest.  (An infinite t stays one, and has no lo.)
@@ -832,7 +833,8 @@ __global__ __launch_bounds__(kExpandTileWaves<RB> * 64, RB < 2 ? 3 : 2) void exp
         }
         if constexpr (HALF) {
             // Halves of t say nothing about infinities: an infinite weight times lo is undefined or of any sign.  Sums that are not finite are made
-            // again from t itself. (It costs 0.1 us of 11.1 for 1024 tokens of prompts, 1024 -> 4096, rank 16; looking for infinite weights before
+            // again from t itself.
+            // (It costs 0.1 us of 11.1 for 1024 tokens of prompts, 1024 -> 4096, rank 16; looking for infinite weights before
             // every product 0.3, and 0.8 of 37 at rank 64.)
             float most = 0.0f;
 #pragma unroll
@@ -926,7 +928,8 @@ template <typename X, typename C, typename W> Plan plan_of(const sparsert_adapte
     // 23 and 29.  Over 405 calls of 8 to 512 tokens, with 2 and 24 adapters, the choices come to 3 % above the best of each.  What they miss is a
     // batch that meets few of many adapters, or many of few: 1024 -> 4096, 1024 tokens, rank 16 in half, tokens and tiles: in runs with 32 adapters
     // 25.9 and 11.5 (tiles), with 64 25.6 and 11.9 (tokens); requests of a token each with 24 26.1 and 32.5 (tiles), with 64 27.0 and 49.7
-    // (tokens); 4096 x 4096, 2048 requests, 64 adapters 73 and 128 (tiles). Tiles are built for ranks up to 64, and for rows of weights that are
+    // (tokens); 4096 x 4096, 2048 requests, 64 adapters 73 and 128 (tiles).
+    // Tiles are built for ranks up to 64, and for rows of weights that are
     // read in pieces (pieces_fit).  Beyond them tokens take what is left: 4096 x 4096, 2048 tokens, half, rank 64 37 us in tiles, 65 601, 96 245,
     // 128 404, 256 716; 1024 -> 4096, rank 8 14.8, 6 17.0, 7 102.
     const double own = (double)d.N * d.batch * ((double)d.M + d.K) * ranks * (int)sizeof(W);
@@ -958,7 +961,7 @@ template <typename X, typename C, typename W> Plan plan_of(const sparsert_adapte
     p.shrink_grid = ((int64_t)d.N + kTokenGroup - 1) / kTokenGroup * p.parts * (ranks / 16); p.shrink_threads = kTokenThreads;
     const int64_t blocks = (d.M + kExpandRows - 1) / kExpandRows;
     int each = 4;
-    // (t of 32 KiB at most in LDS)
+    // (No more tokens than make t 32 KiB in LDS.)
     while (each > 1 && (blocks * (((int64_t)d.N + each * kExpandWaves - 1) / (each * kExpandWaves)) * d.batch < 256 ||
         each * kExpandWaves * ranks > 8192)) each /= 2;
     p.expand = each == 4 ? expand_tokens<C, W, 4>(whole_rank) : each == 2 ? expand_tokens<C, W, 2>(whole_rank) : expand_tokens<C, W, 1>(whole_rank);
