@@ -435,7 +435,8 @@ typedef struct sparsert_norm {
  *                sparsert_adapters take it
  *
  * All of it in binary32, from the unrounded sum h; the results are rounded once.  Half results beyond its range are
- * infinite.  int8: a column with a[n] under 2^-100 (all zeros among them) gives zeros and scale 0; one with an infinite or
+ * infinite.  A floating column whose squares overflow gives zeros, and undefined values where it is infinite.
+ * int8: a column with a[n] under 2^-100 (all zeros among them) gives zeros and scale 0; one with an infinite or
  * undefined h or v, or whose squares overflow, gives zeros and an undefined scale (NaN), which the
  * dequantised product of the column then is as a whole.
  *

@@ -758,3 +758,13 @@ def test_norm_factor_is_rounded_once(K, N, way):
     want = 1 / np.sqrt((1 + x[0, K - 1, :].astype(np.float64) ** 2) / K)
     # one rounding; what is behind it is of the order of its square
     assert (np.abs(y[0, 0, :] - want) <= want * plain.U * (1 + 2.0 ** -20)).all()
+
+
+@pytest.mark.parametrize("K", [90, 9000])
+def test_norm_of_a_floating_column_whose_squares_overflow(K, way):
+    x = np.full((1, K, 20), 1e-3, dtype=np.float32)
+    x[0, 4, 2], x[0, 5, 3], x[0, 6, 3] = 1e25, np.inf, 1e25
+    y, _, _ = run_norm(way, x, None, None, np.float32)
+    sound = [n for n in range(20) if n not in (2, 3)]
+    plain.check_norm(y[..., sound], None, None, x[..., sound], None, None, 1e-5)
+    assert (y[0, :, 2] == 0).all() and np.isnan(y[0, 5, 3]) and (np.delete(y[0, :, 3], 5) == 0).all()
